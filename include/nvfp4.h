@@ -57,7 +57,10 @@ enum { NVFP4_SF_LINEAR = 0, NVFP4_SF_SWIZZLED = 1 };
    closing remark of Appendix B.1: with one global scale per row no separate amax sweep over the whole tensor is needed): global holds rows pairs {amax of the row, s_dec of the row}, Eq. 1 per row,
    Eq. 2-4 unchanged.  Row-wise copies only; nvfp4_quantize makes them in ONE pass and nvfp4_gemm applies the
    vectors in its epilogue (D[i][j] = s_dec^A[i] * s_dec^B[j] * sum ...). */
-enum { NVFP4_FORMAT_NVFP4 = 0, NVFP4_FORMAT_MXFP4 = 1, NVFP4_FORMAT_NVFP4_ROWSCALE = 2 };
+/* MXFP8 is the format of activations that are kept for the backward pass (no operand of nvfp4_gemm): E4M3 elements, one UE8M0
+   power-of-two scale per 32 elements of a row, the smallest 2^E (E >= -127) with amax_b <= 448 * 2^E, no tensor-level scale.
+   Row-wise copies, rounding to nearest; nvfp4_quantize, nvfp4_rmsnorm_fwd and nvfp4_gemm_bf16_epilogue make them. */
+enum { NVFP4_FORMAT_NVFP4 = 0, NVFP4_FORMAT_MXFP4 = 1, NVFP4_FORMAT_NVFP4_ROWSCALE = 2, NVFP4_FORMAT_MXFP8 = 3 };
 enum {
   /* the column-wise copy draws its stochastic-rounding bits from a second stream (bit 63 of
      sr_offset set) instead of sharing the draw of the same source element with the row-wise copy.  Where both copies of
@@ -96,7 +99,9 @@ typedef struct nvfp4_tensor {
   int32_t format;   /* NVFP4_FORMAT_NVFP4 (0) or NVFP4_FORMAT_MXFP4; MXFP4: scales hold rows * cols/32 UE8M0
                        bytes (byte b = 2^(b-127)), same two layouts with 32-element blocks (swizzled needs
                        cols % 128 == 0), global is written as {0, 1} and not used;
-                       NVFP4_FORMAT_NVFP4_ROWSCALE: global is float[2 * rows] */
+                       NVFP4_FORMAT_NVFP4_ROWSCALE: global is float[2 * rows];
+                       NVFP4_FORMAT_MXFP8: codes are rows * cols E4M3 bytes, scales rows * ceil(cols/32) UE8M0 bytes (a row's last
+                       block may be short), linear layout only, cols % 8 == 0, global is not used and may be NULL */
 } nvfp4_tensor;
 
 /*
@@ -141,6 +146,8 @@ typedef struct nvfp4_quant_opts {
  *   MXFP4 blocks likewise, excepted) and no Hadamard transform is allowed.
  *   rowwise->format == NVFP4_FORMAT_NVFP4_ROWSCALE: one pass, colwise must be NULL, block_rows 1, no transform,
  *   bf16 source; rowwise->global receives 2 * rows floats.
+ *   rowwise->format == NVFP4_FORMAT_MXFP8: one pass, colwise must be NULL, block_rows 1, round-to-nearest, no transform; any number
+ *   of rows, cols % 8 == 0, x 16-byte aligned, ld a multiple of 8 (binary32: of 4); the only flag is NVFP4_INPUT_FP32.
  * Two passes over x: a tensor-amax reduction (in the rotated space for a transformed copy),
  * then transform + scale + round + pack.  Stochastic rounding rounds up iff
  * u + 0.5 < 256 * frac, u = the 8-bit Philox draw of the source position, frac = the position of
@@ -293,8 +300,80 @@ NVFP4_API nvfp4_status nvfp4_linear_fwd_noalloc(const void* X, const void* W, in
                                                 void* cuda_stream);
 
 /*
+ * Around the linear layers: what makes their input, follows their product and is kept for their backward pass.
+ * Matrices are row-major with a leading dimension in elements (>= cols); bf16 leading dimensions are multiples of 8, binary32 ones of
+ * 4, pointers 16-byte aligned, cols a multiple of 8.  Any number of rows from one on.  Buffers overlap only where it is said that they may.
+ *
+ * nvfp4_rmsnorm_fwd: h = x + residual (one binary32 addition; h = x without a residual), rstd = 1 / sqrt(mean(h^2) + eps) per row,
+ *   y = h * rstd * gain.  y and the copies are taken of the binary32 h.
+ *   x: bf16.  residual: NULL, bf16 or binary32 (residual_is_fp32).  gain: binary32 [cols] or NULL (ones).  eps > 0.
+ *   h: NULL or the sum in the residual's type (NULL without a residual); may be the residual itself (same leading dimension).
+ *   y: NULL or bf16; may be x itself (same leading dimension).  y8, h8: NULL or NVFP4_FORMAT_MXFP8 copies of y and h.
+ *   rstd: NULL or binary32 [rows].  At least one output.
+ * nvfp4_rmsnorm_bwd: with n = h * rstd and g = dy * gain:  dh = rstd * (g - n * mean(g * n)) + residual_grad,
+ *   dgain = (accumulate_dgain ? dgain : 0) + sum over the rows of dy * n.
+ *   h as it was kept: bf16 or binary32 (h_is_fp32), or, h == NULL, its MXFP8 copy h8 (exactly one of the two).  rstd as the forward call
+ *   wrote it.  residual_grad: NULL, or the gradient that reaches h along the residual path, in dh's type (dh_is_fp32); dh may be
+ *   residual_grad itself (same leading dimension).  dgain: NULL or binary32 [cols].
+ *   workspace: nvfp4_rmsnorm_bwd_workspace_bytes(rows, cols), 256-byte aligned; may be NULL without dgain for cols <= 20480.
+ *   The order of every sum depends on the sizes and the GPU alone.
+ */
+NVFP4_API nvfp4_status nvfp4_rmsnorm_fwd(const void* x_bf16, int64_t ldx, const void* residual, int64_t ldr,
+                                         int32_t residual_is_fp32, const float* gain, int64_t rows, int64_t cols, float eps,
+                                         void* h, int64_t ldh, void* y_bf16, int64_t ldy, const nvfp4_tensor* y8,
+                                         const nvfp4_tensor* h8, float* rstd, void* cuda_stream);
+NVFP4_API size_t nvfp4_rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+NVFP4_API nvfp4_status nvfp4_rmsnorm_bwd(const void* dy_bf16, int64_t lddy, const void* h, int64_t ldh, int32_t h_is_fp32,
+                                         const nvfp4_tensor* h8, const float* gain, const float* rstd, int64_t rows,
+                                         int64_t cols, const void* residual_grad, int64_t ldrg, void* dh, int64_t lddh,
+                                         int32_t dh_is_fp32, float* dgain, int32_t accumulate_dgain, void* workspace,
+                                         size_t workspace_bytes, void* cuda_stream);
+
+/* Activations: none; max(z, 0)^2 (the recipe's squared ReLU); z / (1 + e^-z); z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+enum { NVFP4_ACT_NONE = 0, NVFP4_ACT_RELU2 = 1, NVFP4_ACT_SILU = 2, NVFP4_ACT_GELU = 3 };
+
+/* What follows a product: z = A B^T + bias, D = act(z) + residual, and z kept for nvfp4_act_bwd. */
+typedef struct nvfp4_epilogue {
+  const float* bias;        /* NULL or binary32 [N]                                                                  */
+  const void* residual;     /* NULL or bf16 [M x N], leading dimension ldr; may be D itself (same leading dimension) */
+  int64_t ldr;
+  void* z_bf16;             /* NULL or bf16 [M x N], leading dimension ldz                                           */
+  int64_t ldz;
+  const nvfp4_tensor* z8;   /* NULL or an NVFP4_FORMAT_MXFP8 copy [M x N]; not beside z_bf16                          */
+  int32_t act;              /* NVFP4_ACT_...                                                                         */
+  int32_t reserved;         /* 0                                                                                     */
+} nvfp4_epilogue;
+/*
+ * nvfp4_gemm_bf16_epilogue: the product of nvfp4_gemm_bf16 for K-major operands (X [M x K], W [N x K]) with the above in its epilogue,
+ *   in binary32 until D (bf16) is rounded.  M any number from one on; N, K multiples of 8; lda, ldb, ldd, ldr, ldz multiples of 8; pointers
+ *   16-byte aligned.
+ * nvfp4_act_bwd: dz = da * act'(z) (bf16), a = act(z) (bf16: the next layer's input made again for its weight gradient),
+ *   dbias = (accumulate_dbias ? dbias : 0) + sum over the rows of dz before its rounding.
+ *   z: bf16, or, z == NULL, its MXFP8 copy z8 (exactly one of the two; neither with NVFP4_ACT_NONE and a == NULL).  dz, a, dbias: each may
+ *   be NULL, not all; dz may be da itself and a may be z itself (same leading dimensions).
+ *   workspace: nvfp4_act_bwd_workspace_bytes(rows, cols), 256-byte aligned, for dbias (NULL without).
+ * nvfp4_linear_bf16_bwd8: nvfp4_linear_bf16_bwd with X from its MXFP8 copy [M x K]: dW = dY^T X^, X^ the copy's values in bf16 (exact
+ *   but below 2^-126).  Same bits as nvfp4_dequantize_bf16 followed by nvfp4_linear_bf16_bwd.
+ *   workspace: nvfp4_linear_bf16_bwd8_workspace_bytes(M, K), 256-byte aligned, for X^ (NULL without dW).
+ * nvfp4_dequantize_bf16: the values of an MXFP8 copy in bf16, leading dimension ld.
+ */
+NVFP4_API nvfp4_status nvfp4_gemm_bf16_epilogue(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N,
+                                                int64_t K, const nvfp4_epilogue* epilogue, void* D_bf16, int64_t ldd,
+                                                void* cuda_stream);
+NVFP4_API size_t nvfp4_act_bwd_workspace_bytes(int64_t rows, int64_t cols);
+NVFP4_API nvfp4_status nvfp4_act_bwd(const void* da_bf16, int64_t ldda, const void* z_bf16, int64_t ldz,
+                                     const nvfp4_tensor* z8, int32_t act, int64_t rows, int64_t cols, void* dz_bf16,
+                                     int64_t lddz, void* a_bf16, int64_t lda, float* dbias, int32_t accumulate_dbias,
+                                     void* workspace, size_t workspace_bytes, void* cuda_stream);
+NVFP4_API size_t nvfp4_linear_bf16_bwd8_workspace_bytes(int64_t M, int64_t K);
+NVFP4_API nvfp4_status nvfp4_linear_bf16_bwd8(const void* dY, const nvfp4_tensor* X8, const void* W, int64_t M, int64_t N,
+                                              int64_t K, void* dX_bf16, float* dW_fp32, int32_t accumulate_dw, void* workspace,
+                                              size_t workspace_bytes, void* cuda_stream);
+NVFP4_API nvfp4_status nvfp4_dequantize_bf16(const nvfp4_tensor* t, void* out_bf16, int64_t ld, void* cuda_stream);
+
+/*
  * Test aids (not on the hot path).
- * nvfp4_dequantize: out[r][c] = code * fp32(block scale) * s_dec as fp32 (the decode of Section 2).
+ * nvfp4_dequantize: out[r][c] = code * fp32(block scale) * s_dec as fp32 (the decode of Section 2), any format.
  * nvfp4_rht16: the transformed values y = x*(S*H_16) of the row-wise (colwise == 0, out [rows x cols])
  *   or column-wise (colwise != 0, out [cols x rows]) copy, fp32, as the quantizer sees them.
  * nvfp4_e2m1_sr: codes[i] = the E2M1 code (4 bits in a byte) of the already scaled value v[i] under the

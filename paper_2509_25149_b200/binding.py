@@ -19,7 +19,8 @@ OK = 0
 ROUND_NEAREST_EVEN, ROUND_STOCHASTIC = 0, 1
 SF_LINEAR, SF_SWIZZLED = 0, 1
 SR_INDEPENDENT_COPIES, AMAX_PROVIDED, INPUT_FP32, LINEAR_ROW_SCALES = 1, 2, 4, 8
-FORMAT_NVFP4, FORMAT_MXFP4, FORMAT_NVFP4_ROWSCALE = 0, 1, 2
+FORMAT_NVFP4, FORMAT_MXFP4, FORMAT_NVFP4_ROWSCALE, FORMAT_MXFP8 = 0, 1, 2, 3
+ACT_NONE, ACT_RELU2, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 EXPORTED = (
     "nvfp4_quantize", "nvfp4_gemm", "nvfp4_linear_fwd_workspace_bytes", "nvfp4_linear_bwd_workspace_bytes",
@@ -28,6 +29,9 @@ EXPORTED = (
     "nvfp4_set_gemm_tile_n", "nvfp4_gemm_tile", "nvfp4_set_gemm_experiment", "nvfp4_status_string", "nvfp4_launch_count",
     "nvfp4_linear_fwd_noalloc", "nvfp4_linear_fwd_noalloc_max_bytes",
     "nvfp4_gemm_bf16", "nvfp4_linear_bf16_fwd", "nvfp4_linear_bf16_bwd", "nvfp4_quant_error", "nvfp4_sq_error",
+    "nvfp4_dequantize_bf16", "nvfp4_rmsnorm_fwd", "nvfp4_rmsnorm_bwd_workspace_bytes", "nvfp4_rmsnorm_bwd",
+    "nvfp4_gemm_bf16_epilogue", "nvfp4_act_bwd_workspace_bytes", "nvfp4_act_bwd", "nvfp4_linear_bf16_bwd8_workspace_bytes",
+    "nvfp4_linear_bf16_bwd8",
 )
 
 
@@ -87,6 +91,20 @@ def lib() -> ctypes.CDLL:
         L.nvfp4_quant_error.restype, L.nvfp4_quant_error.argtypes = i32, [vp, i64, i64, i64, TP, vp, vp]
         L.nvfp4_sq_error.restype = i32
         L.nvfp4_sq_error.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, vp, vp]
+        sz, f32 = c.c_size_t, c.c_float
+        L.nvfp4_dequantize_bf16.restype, L.nvfp4_dequantize_bf16.argtypes = i32, [TP, vp, i64, vp]
+        L.nvfp4_rmsnorm_fwd.restype = i32
+        L.nvfp4_rmsnorm_fwd.argtypes = [vp, i64, vp, i64, i32, vp, i64, i64, f32, vp, i64, vp, i64, TP, TP, vp, vp]
+        L.nvfp4_rmsnorm_bwd.restype = i32
+        L.nvfp4_rmsnorm_bwd.argtypes = [vp, i64, vp, i64, i32, TP, vp, vp, i64, i64, vp, i64, vp, i64, i32, vp, i32, vp, sz, vp]
+        L.nvfp4_gemm_bf16_epilogue.restype = i32
+        L.nvfp4_gemm_bf16_epilogue.argtypes = [vp, i64, vp, i64, i64, i64, i64, vp, vp, i64, vp]
+        L.nvfp4_act_bwd.restype = i32
+        L.nvfp4_act_bwd.argtypes = [vp, i64, vp, i64, TP, i32, i64, i64, vp, i64, vp, i64, vp, i32, vp, sz, vp]
+        L.nvfp4_linear_bf16_bwd8.restype, L.nvfp4_linear_bf16_bwd8.argtypes = i32, [vp, TP, vp, i64, i64, i64, vp, vp, i32, vp, sz, vp]
+        for name in ("nvfp4_rmsnorm_bwd", "nvfp4_act_bwd", "nvfp4_linear_bf16_bwd8"):
+            fn = getattr(L, name + "_workspace_bytes")
+            fn.restype, fn.argtypes = sz, [i64, i64]
         L.nvfp4_dequantize.restype, L.nvfp4_dequantize.argtypes = i32, [TP, vp, vp]
         L.nvfp4_rht16.restype, L.nvfp4_rht16.argtypes = i32, [vp, i64, i64, i64, i32, u32, vp, vp]
         L.nvfp4_e2m1_sr.restype, L.nvfp4_e2m1_sr.argtypes = i32, [vp, vp, i64, vp, vp]
@@ -129,6 +147,10 @@ def _stream() -> int:
     return _raw_stream(_get_device())
 
 
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return t.data_ptr() if t is not None else None
+
+
 _TENSOR_FIELDS = struct.Struct("PPPqqii")  # nvfp4_tensor
 assert _TENSOR_FIELDS.size == ctypes.sizeof(CTensor)
 
@@ -138,24 +160,28 @@ class NVFP4Tensor:
     """Device buffers of one quantized copy ([rows x cols], cols = contraction dimension)."""
     codes: torch.Tensor   # uint8 [rows, cols/2]
     scales: torch.Tensor  # uint8 [rows * cols/16] (linear: viewable as [rows, cols/16])
-    glob: torch.Tensor    # float32 [2] = {amax, s_dec}
+    glob: Optional[torch.Tensor]  # float32 [2] = {amax, s_dec}
     rows: int
     cols: int
     sf_layout: int = SF_SWIZZLED
     format: int = FORMAT_NVFP4  # FORMAT_MXFP4: scales are rows * cols/32 UE8M0 bytes, glob unused ({0, 1})
+    # FORMAT_MXFP8: codes uint8 [rows, cols] (E4M3), scales uint8 [rows, ceil(cols/32)] (UE8M0), glob unused (may be None), SF_LINEAR
 
     def c(self) -> CTensor:
-        return CTensor(self.codes.data_ptr(), self.scales.data_ptr(), self.glob.data_ptr(), self.rows, self.cols,
+        return CTensor(self.codes.data_ptr(), self.scales.data_ptr(), _ptr(self.glob), self.rows, self.cols,
                        self.sf_layout, self.format)
 
     def packed(self) -> bytes:
         """The C struct as bytes; ctypes passes their address.  Half the host time of building a ctypes structure."""
-        return _TENSOR_FIELDS.pack(self.codes.data_ptr(), self.scales.data_ptr(), self.glob.data_ptr(), self.rows,
+        return _TENSOR_FIELDS.pack(self.codes.data_ptr(), self.scales.data_ptr(), _ptr(self.glob) or 0, self.rows,
                                    self.cols, self.sf_layout, self.format)
 
 
 def alloc_tensor(rows: int, cols: int, sf_layout: int = SF_SWIZZLED, device="cuda",
                  format: int = FORMAT_NVFP4) -> NVFP4Tensor:
+    if format == FORMAT_MXFP8:  # (row by row whatever the layout asked for: it is no operand of the block-scaled product)
+        return NVFP4Tensor(torch.empty((rows, cols), dtype=torch.uint8, device=device),
+                           torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device=device), None, rows, cols, SF_LINEAR, format)
     block = 32 if format == FORMAT_MXFP4 else 16
     glob = torch.zeros((2 * rows if format == FORMAT_NVFP4_ROWSCALE else 2,), dtype=torch.float32, device=device)
     if format == FORMAT_MXFP4:
@@ -316,6 +342,125 @@ def nvfp4_dequantize(t: NVFP4Tensor, out: Optional[torch.Tensor] = None) -> torc
         out = torch.empty((t.rows, t.cols), dtype=torch.float32, device=t.codes.device)
     _check(lib().nvfp4_dequantize(_ref(t), out.data_ptr(), _stream()), "nvfp4_dequantize")
     return out
+
+
+# ---- around the linear layers -------------------------------------------------------------------------------------------
+_BF16_OR_FP32 = (torch.bfloat16, torch.float32)
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, *dtypes) -> int:
+    """Checks a row-major matrix and returns its leading dimension."""
+    assert t.is_cuda and t.dtype in dtypes and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols
+    assert t.stride(1) == 1
+    return t.stride(0) if rows > 1 else cols  # (a single row's stride says nothing)
+
+
+def _vector(t: Optional[torch.Tensor], n: int) -> Optional[int]:
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float32 and t.dim() == 1 and t.shape[0] == n and (n == 1 or t.stride(0) == 1)
+    return t.data_ptr()
+
+
+def nvfp4_dequantize_bf16(t: NVFP4Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values of an MXFP8 copy in bf16."""
+    if out is None:
+        out = torch.empty((t.rows, t.cols), dtype=torch.bfloat16, device=t.codes.device)
+    _check(lib().nvfp4_dequantize_bf16(t.packed(), out.data_ptr(), _matrix(out, t.rows, t.cols, torch.bfloat16), _stream()),
+           "nvfp4_dequantize_bf16")
+    return out
+
+
+def nvfp4_rmsnorm_fwd(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, y: Optional[torch.Tensor] = None,
+                      rstd: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                      h: Optional[torch.Tensor] = None, y8: Optional[NVFP4Tensor] = None,
+                      h8: Optional[NVFP4Tensor] = None) -> None:
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain; y8, h8: MXFP8 copies of y and h."""
+    rows, cols = x.shape
+    fp32 = residual is not None and residual.dtype == torch.float32
+    assert h is None or residual is None or h.dtype == residual.dtype
+    _check(lib().nvfp4_rmsnorm_fwd(
+        x.data_ptr(), _matrix(x, rows, cols, torch.bfloat16), _ptr(residual),
+        _matrix(residual, rows, cols, *_BF16_OR_FP32) if residual is not None else 0, fp32, _vector(gain, cols), rows, cols, eps,
+        _ptr(h), _matrix(h, rows, cols, *_BF16_OR_FP32) if h is not None else 0,
+        _ptr(y), _matrix(y, rows, cols, torch.bfloat16) if y is not None else 0, _ref(y8), _ref(h8), _vector(rstd, rows), _stream()),
+        "nvfp4_rmsnorm_fwd")
+
+
+def nvfp4_rmsnorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().nvfp4_rmsnorm_bwd_workspace_bytes(rows, cols))
+
+
+def nvfp4_rmsnorm_bwd(dy: torch.Tensor, h, gain: Optional[torch.Tensor], rstd: torch.Tensor, dh: torch.Tensor,
+                      dgain: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      residual_grad: Optional[torch.Tensor] = None, accumulate_dgain: bool = False) -> None:
+    """h: the kept sum, a bf16 or binary32 tensor or its MXFP8 copy."""
+    rows, cols = dy.shape
+    copy = isinstance(h, NVFP4Tensor)
+    assert residual_grad is None or residual_grad.dtype == dh.dtype
+    _check(lib().nvfp4_rmsnorm_bwd(
+        dy.data_ptr(), _matrix(dy, rows, cols, torch.bfloat16), None if copy else h.data_ptr(),
+        0 if copy else _matrix(h, rows, cols, *_BF16_OR_FP32), not copy and h.dtype == torch.float32, h.packed() if copy else None,
+        _vector(gain, cols), _vector(rstd, rows), rows, cols, _ptr(residual_grad),
+        _matrix(residual_grad, rows, cols, *_BF16_OR_FP32) if residual_grad is not None else 0,
+        dh.data_ptr(), _matrix(dh, rows, cols, *_BF16_OR_FP32), dh.dtype == torch.float32, _vector(dgain, cols), accumulate_dgain,
+        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nvfp4_rmsnorm_bwd")
+
+
+_EPILOGUE_FIELDS = struct.Struct("PPqPqPii")  # nvfp4_epilogue
+
+
+def nvfp4_gemm_bf16_epilogue(A: torch.Tensor, B: torch.Tensor, D: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                             act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, z=None) -> None:
+    """z = A B^T + bias, D = act(z) + residual (A [M x K], B [N x K]); z: a bf16 tensor or an MXFP8 copy that is to keep it."""
+    M, N = D.shape
+    K = A.shape[1]
+    copy = z.packed() if isinstance(z, NVFP4Tensor) else None
+    plain_z = z if copy is None else None
+    held = ctypes.c_char_p(copy)  # (the struct's address; held until the call returns)
+    epilogue = _EPILOGUE_FIELDS.pack(
+        _vector(bias, N) or 0, _ptr(residual) or 0, _matrix(residual, M, N, torch.bfloat16) if residual is not None else 0,
+        _ptr(plain_z) or 0, _matrix(plain_z, M, N, torch.bfloat16) if plain_z is not None else 0,
+        (ctypes.cast(held, ctypes.c_void_p).value or 0) if copy is not None else 0, act, 0)
+    _check(lib().nvfp4_gemm_bf16_epilogue(A.data_ptr(), _matrix(A, M, K, torch.bfloat16), B.data_ptr(),
+                                          _matrix(B, N, K, torch.bfloat16), M, N, K, epilogue, D.data_ptr(),
+                                          _matrix(D, M, N, torch.bfloat16), _stream()), "nvfp4_gemm_bf16_epilogue")
+
+
+def nvfp4_act_bwd_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().nvfp4_act_bwd_workspace_bytes(rows, cols))
+
+
+def nvfp4_act_bwd(da: torch.Tensor, z, act: int, dz: Optional[torch.Tensor] = None, a: Optional[torch.Tensor] = None,
+                  dbias: Optional[torch.Tensor] = None, accumulate_dbias: bool = False,
+                  workspace: Optional[torch.Tensor] = None) -> None:
+    """dz = da act'(z), a = act(z), dbias = column sums of dz; z: a bf16 tensor, its MXFP8 copy, or None where nothing needs it."""
+    rows, cols = da.shape
+    copy = isinstance(z, NVFP4Tensor)
+    plain_z = None if copy else z
+    ld = lambda t: _matrix(t, rows, cols, torch.bfloat16) if t is not None else 0
+    _check(lib().nvfp4_act_bwd(
+        da.data_ptr(), ld(da), _ptr(plain_z), ld(plain_z), z.packed() if copy else None, act, rows, cols, _ptr(dz), ld(dz), _ptr(a),
+        ld(a), _vector(dbias, cols), accumulate_dbias, _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nvfp4_act_bwd")
+
+
+def nvfp4_linear_bf16_bwd8_workspace_bytes(M: int, K: int) -> int:
+    return int(lib().nvfp4_linear_bf16_bwd8_workspace_bytes(M, K))
+
+
+def nvfp4_linear_bf16_bwd8(dY: torch.Tensor, X8: Optional[NVFP4Tensor], W: Optional[torch.Tensor], dX: Optional[torch.Tensor],
+                           dW: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, accumulate_dw: bool = False) -> None:
+    """Both gradients of a BF16 layer whose input was kept as an MXFP8 copy."""
+    M, N = dY.shape
+    K = X8.cols if X8 is not None else W.shape[1]
+    assert dY.is_cuda and dY.is_contiguous() and dY.dtype == torch.bfloat16
+    assert dX is None or (W is not None and W.is_contiguous() and W.dtype == torch.bfloat16 and tuple(W.shape) == (N, K)
+                          and dX.is_contiguous() and dX.dtype == torch.bfloat16 and tuple(dX.shape) == (M, K))
+    assert dW is None or (X8 is not None and dW.is_contiguous() and dW.dtype == torch.float32 and tuple(dW.shape) == (N, K))
+    _check(lib().nvfp4_linear_bf16_bwd8(dY.data_ptr(), _ref(X8), _ptr(W), M, N, K, _ptr(dX), _ptr(dW), int(accumulate_dw),
+                                        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                        _stream()), "nvfp4_linear_bf16_bwd8")
 
 
 def nvfp4_rht16(x: torch.Tensor, colwise: bool, sign_mask: int) -> torch.Tensor:

@@ -2,6 +2,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "around.h"
 #include "common.cuh"
 #include "gemm.h"
 #include "quantize.h"
@@ -20,8 +21,6 @@ using namespace nvfp4;
 static __device__ __align__(256) unsigned char g_noalloc_scratch[NVFP4_NOALLOC_SCRATCH_BYTES];
 
 namespace {
-
-inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 nvfp4_status check_copy(const nvfp4_tensor* t, int64_t rows, int64_t cols) {
   if (!t->codes || !t->scales || !t->global) return NVFP4_ERR_NULL;
@@ -74,6 +73,18 @@ float2* parts_in(void* out, int64_t out_bytes, const void* in0, int64_t bytes0, 
   return apart(in0, bytes0) && apart(in1, bytes1) ? static_cast<float2*>(out) : nullptr;
 }
 
+nvfp4_status quantize8_impl(const void* x, int64_t rows, int64_t cols, int64_t ld, const nvfp4_quant_opts* o, const nvfp4_tensor* q,
+                            const nvfp4_tensor* colwise, cudaStream_t s) {
+  if (colwise || o->block_rows != 1 || o->rht_rowwise || o->rht_colwise || o->rounding != NVFP4_ROUND_NEAREST_EVEN) return NVFP4_ERR_ARG;
+  if (o->flags & ~NVFP4_INPUT_FP32) return NVFP4_ERR_ARG;
+  const bool fp32 = (o->flags & NVFP4_INPUT_FP32) != 0;
+  if (rows <= 0 || cols <= 0 || rows > (int64_t)1 << 30 || cols > (int64_t)1 << 30 || cols % 8 != 0 || ld < cols) return NVFP4_ERR_SHAPE;
+  if (ld % (fp32 ? 4 : 8) != 0 || !aligned(x, 16)) return NVFP4_ERR_ALIGN;
+  const nvfp4_status st = check_copy8(q, rows, cols);
+  if (st != NVFP4_OK) return st;
+  return launch_quantize8(x, fp32, rows, cols, ld, *q, s) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
+}
+
 // parts: room for pass 1's maxima if it may leave them in parts (an activation or a gradient of a layer).
 // check_only: every argument check of the call, no launch (the composed calls validate all their steps first, so
 // that a rejected call has enqueued nothing)
@@ -82,6 +93,7 @@ nvfp4_status quantize_impl(const void* x, int64_t rows, int64_t cols, int64_t ld
                            bool check_only = false, float2* parts = nullptr) {
   if (!x || !o) return NVFP4_ERR_NULL;
   if (!rowwise && !colwise) return NVFP4_ERR_NULL;
+  if (rowwise && rowwise->format == NVFP4_FORMAT_MXFP8) return quantize8_impl(x, rows, cols, ld, o, rowwise, colwise, s);
   if (rows <= 0 || cols <= 0 || rows % 16 != 0 || cols % 16 != 0) return NVFP4_ERR_SHAPE;
   if (ld < cols) return NVFP4_ERR_SHAPE;
   if (ld % 16 != 0 || !aligned(x, 32)) return NVFP4_ERR_ALIGN;
@@ -252,6 +264,37 @@ nvfp4_status bf16_prepare(const void* A, int32_t a_layout, int64_t lda, const vo
   g.M = (int)M; g.N = (int)N; g.K = (int)K;
   g.a_mn = a_layout == NVFP4_MN_MAJOR; g.b_mn = b_layout == NVFP4_MN_MAJOR;
   g.d_is_fp32 = d_is_fp32 != 0; g.accumulate = accumulate != 0;
+  return NVFP4_OK;
+}
+
+// argument checks of a product with an epilogue and their launch descriptions
+nvfp4_status epilogue_prepare(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K,
+                              const nvfp4_epilogue* e, void* D, int64_t ldd, DenseGemmArgs& g, EpilogueArgs& ea) {
+  if (!A || !B || !e || !D) return NVFP4_ERR_NULL;
+  if (M <= 0 || N <= 0 || K <= 0 || N % 8 != 0 || K % 8 != 0) return NVFP4_ERR_SHAPE;
+  if (M > 0x7fffff00 || N > 0x7fffff00 || K > 0x7fffff00 || ((M + 255) / 256) * ((N + 127) / 128) > 0x7fffffff) return NVFP4_ERR_SHAPE;
+  if (lda < K || ldb < K || ldd < N || (e->residual && e->ldr < N) || (e->z_bf16 && e->ldz < N)) return NVFP4_ERR_SHAPE;
+  if (e->act < NVFP4_ACT_NONE || e->act > NVFP4_ACT_GELU || e->reserved != 0 || (e->z_bf16 && e->z8)) return NVFP4_ERR_ARG;
+  if (lda % 8 != 0 || ldb % 8 != 0 || ldd % 8 != 0 || !aligned(A, 16) || !aligned(B, 16) || !aligned(D, 16) || !aligned(e->bias, 16) ||
+      (e->residual && (e->ldr % 8 != 0 || !aligned(e->residual, 16))) || (e->z_bf16 && (e->ldz % 8 != 0 || !aligned(e->z_bf16, 16))))
+    return NVFP4_ERR_ALIGN;
+  if (e->z8) {
+    const nvfp4_status st = check_copy8(e->z8, M, N);
+    if (st != NVFP4_OK) return st;
+  }
+  g = DenseGemmArgs{};
+  g.a = A; g.b = B; g.d = D;
+  g.lda = lda; g.ldb = ldb; g.ldd = ldd;
+  g.M = (int)M; g.N = (int)N; g.K = (int)K;
+  ea = EpilogueArgs{};
+  ea.bias = e->bias;
+  ea.residual = e->residual; ea.ldr = e->ldr;
+  ea.z = e->z_bf16; ea.ldz = e->ldz;
+  if (e->z8) {
+    ea.z8_codes = e->z8->codes;
+    ea.z8_scales = e->z8->scales;
+  }
+  ea.act = e->act;
   return NVFP4_OK;
 }
 
@@ -504,6 +547,40 @@ nvfp4_status nvfp4_linear_bf16_bwd(const void* dY, const void* X, const void* W,
   return bf16_impl(dgrad_first ? gd : gw, both ? (dgrad_first ? &gw : &gd) : nullptr, cuda_stream);
 }
 
+nvfp4_status nvfp4_gemm_bf16_epilogue(const void* A, int64_t lda, const void* B, int64_t ldb, int64_t M, int64_t N, int64_t K,
+                                      const nvfp4_epilogue* epilogue, void* D_bf16, int64_t ldd, void* cuda_stream) {
+  DenseGemmArgs g;
+  EpilogueArgs e;
+  const nvfp4_status st = epilogue_prepare(A, lda, B, ldb, M, N, K, epilogue, D_bf16, ldd, g, e);
+  if (st != NVFP4_OK) return st;
+  Bf16Wide wide;
+  const int tile = bf16_tile(g, nullptr, g_tile_n.load(std::memory_order_relaxed), &wide);
+  return launch_gemm_bf16_epilogue(g, e, tile, wide, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
+}
+
+size_t nvfp4_linear_bf16_bwd8_workspace_bytes(int64_t M, int64_t K) { return M > 0 && K > 0 ? align_up((size_t)M * (size_t)K * 2, 256) : 0; }
+
+nvfp4_status nvfp4_linear_bf16_bwd8(const void* dY, const nvfp4_tensor* X8, const void* W, int64_t M, int64_t N, int64_t K,
+                                    void* dX_bf16, float* dW_fp32, int32_t accumulate_dw, void* workspace, size_t workspace_bytes,
+                                    void* cuda_stream) {
+  if (!dY) return NVFP4_ERR_NULL;
+  if (!dX_bf16 && !dW_fp32) return NVFP4_ERR_NULL;
+  if (dW_fp32 && !X8) return NVFP4_ERR_NULL;
+  if (M <= 0 || N <= 0 || K <= 0 || M > 0x7fffff00 || N > 0x7fffff00 || K > 0x7fffff00) return NVFP4_ERR_SHAPE;
+  nvfp4_status st;
+  DenseGemmArgs g;  // every step is validated before the first launch
+  if (dX_bf16 && (st = bf16_prepare(dY, NVFP4_K_MAJOR, N, W, NVFP4_MN_MAJOR, K, M, K, N, dX_bf16, 0, K, 0, g)) != NVFP4_OK) return st;
+  if (dW_fp32) {
+    if ((st = check_copy8(X8, M, K)) != NVFP4_OK) return st;
+    if (!workspace || workspace_bytes < nvfp4_linear_bf16_bwd8_workspace_bytes(M, K)) return NVFP4_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return NVFP4_ERR_ALIGN;
+    if ((st = bf16_prepare(dY, NVFP4_MN_MAJOR, N, workspace, NVFP4_MN_MAJOR, K, N, K, M, dW_fp32, 1, K, accumulate_dw, g)) != NVFP4_OK)
+      return st;
+    if (launch_dequantize8(*X8, workspace, false, K, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return NVFP4_ERR_CUDA;
+  }
+  return nvfp4_linear_bf16_bwd(dY, workspace, W, M, N, K, dX_bf16, dW_fp32, accumulate_dw, cuda_stream);
+}
+
 nvfp4_status nvfp4_quant_error(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, const nvfp4_tensor* q,
                                double* out2, void* cuda_stream) {
   if (!x_bf16 || !q || !out2) return NVFP4_ERR_NULL;
@@ -532,6 +609,13 @@ nvfp4_status nvfp4_sq_error(const void* ref, int32_t ref_is_fp32, int64_t ld_ref
 }
 
 nvfp4_status nvfp4_dequantize(const nvfp4_tensor* t, float* out, void* cuda_stream) {
+  if (t && t->format == NVFP4_FORMAT_MXFP8) {
+    if (!out) return NVFP4_ERR_NULL;
+    const nvfp4_status st8 = check_copy8(t, t->rows, t->cols);
+    if (st8 != NVFP4_OK) return st8;
+    if (!aligned(out, 16)) return NVFP4_ERR_ALIGN;
+    return launch_dequantize8(*t, out, true, t->cols, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
+  }
   if (!t || !out || !t->codes || !t->scales || !t->global) return NVFP4_ERR_NULL;
   nvfp4_status st = check_copy(t, t->rows, t->cols);
   if (st != NVFP4_OK) return st;

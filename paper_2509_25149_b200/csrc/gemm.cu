@@ -743,11 +743,12 @@ static bool make_bf16_maps(const DenseGemmArgs& g, CUtensorMap* m) {  // A, B, D
 
 static int bf16_tiles(const DenseGemmArgs& g, int bn) { return ((g.M + 255) / 256) * ((g.N + bn - 1) / bn); }
 
-template <int BN, int SPLIT, bool TWO>
+template <int BN, int SPLIT, bool TWO, class E = dense::NoEpilogue>
 static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemmArgs* g1, const Bf16Wide& wide_cols, int max_pairs,
-                                        cudaStream_t s) {
-  auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO>;
-  constexpr int smem = dense::Cfg<BN, SPLIT>::kSmemBytes;
+                                        cudaStream_t s, const E& epilogue = E{}) {
+  auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO, E>;
+  constexpr int smem = dense::Cfg<BN, SPLIT>::kSmemBytes + E::kSmemBytes;
+  static_assert(smem <= 232448, "shared memory budget");
   CUtensorMap m[6];
   if (!make_bf16_maps<BN, SPLIT>(g0, m)) return cudaErrorInvalidValue;
   if (g1) {
@@ -784,9 +785,28 @@ static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemm
   }
   const int pairs = a.n_tiles < max_pairs || SPLIT > 1 ? a.n_tiles : max_pairs;  // SPLIT > 1: a cluster for each tile
   const cudaError_t e = launch_kernel(kern, dim3(2 * SPLIT * pairs), dim3(dense::kThreads), smem, s, m[0], m[1], m[2],
-                                      m[3], m[4], m[5], a);
+                                      m[3], m[4], m[5], a, epilogue);
   count_launch();
   return e;
+}
+
+template <int BN, int SPLIT = 1>
+static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& a, const Bf16Wide& wide_cols, int max_pairs,
+                                        cudaStream_t s) {
+  dense::Epilogue e{};
+  auto map_of = [&](CUtensorMap* map, const void* p, int64_t ld) {
+    return make_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, (uint64_t)g.N, (uint64_t)g.M, (uint64_t)ld * 2, SPLIT == 4 ? 32 : 64,
+                       128, SPLIT == 4 ? 2 : 1);
+  };
+  if ((a.residual && !map_of(&e.map_r, a.residual, a.ldr)) || (a.z && !map_of(&e.map_z, a.z, a.ldz))) return cudaErrorInvalidValue;
+  e.bias = a.bias;
+  e.z8_codes = a.z8_codes;
+  e.z8_scales = a.z8_scales;
+  e.z8_blocks = (g.N + 31) / 32;
+  e.act = a.act;
+  e.has_residual = a.residual != nullptr;
+  e.has_z = a.z != nullptr;
+  return launch_bf16_problems<BN, SPLIT, false, dense::Epilogue>(g, nullptr, wide_cols, max_pairs, s, e);
 }
 
 // g1 == nullptr: one problem
@@ -846,6 +866,17 @@ cudaError_t launch_gemm_bf16(const DenseGemmArgs& g0, const DenseGemmArgs* g1, i
   if (tile == kTileSplit2) return launch_bf16_t<128, 2>(g0, g1, wide, pairs, s);
   if (tile == kTilePair128) return launch_bf16_t<128>(g0, g1, wide, pairs, s);
   return tile == kTileDouble ? launch_bf16_t<512>(g0, g1, wide, pairs, s) : launch_bf16_t<256>(g0, g1, wide, pairs, s);
+}
+
+cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& e, int tile, const Bf16Wide& wide, cudaStream_t s) {
+  int num_sms = 0;
+  const cudaError_t err = sm_count(&num_sms);
+  if (err != cudaSuccess) return err;
+  const int pairs = num_sms / 2;
+  if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4>(g, e, wide, pairs, s);
+  if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2>(g, e, wide, pairs, s);
+  if (tile == kTilePair128) return launch_bf16_epilogue<128>(g, e, wide, pairs, s);
+  return tile == kTileDouble ? launch_bf16_epilogue<512>(g, e, wide, pairs, s) : launch_bf16_epilogue<256>(g, e, wide, pairs, s);
 }
 
 // Test aid: one warp waits, with the given limit, on a barrier nobody arrives at.  The wait runs out, the code lands

@@ -76,6 +76,17 @@ struct DenseGemmArgs {
 // The tile of such a launch: kTilePair256, kTilePair128, kTileDouble (*wide: how many column tiles of each product are 512 wide) or a
 // split one (`forced`, where every share has a k-block, or by size)
 int bf16_tile(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int forced, Bf16Wide* wide);
+// What follows a product (nvfp4_gemm_bf16_epilogue): z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits
+struct EpilogueArgs {
+  const float* bias;
+  const void* residual;
+  void* z;
+  int64_t ldr, ldz;
+  uint8_t* z8_codes;
+  uint8_t* z8_scales;
+  int act;
+};
+cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& e, int tile, const Bf16Wide& wide, cudaStream_t s);
 cudaError_t launch_gemm_bf16(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, const Bf16Wide& wide, cudaStream_t s);
 
 }  // namespace nvfp4

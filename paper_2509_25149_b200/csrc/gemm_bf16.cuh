@@ -17,6 +17,8 @@
 // Included by gemm.cu only.
 #pragma once
 
+#include "act.cuh"
+#include "copy8.cuh"
 #include "gemm_2cta.cuh"
 
 namespace nvfp4 {
@@ -53,6 +55,141 @@ struct Args {
   int seg_end[4];
 };
 
+// What follows a product: z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits (a launch with one problem)
+struct NoEpilogue {
+  static constexpr bool kFused = false;
+  static constexpr int kSmemBytes = 0;
+};
+struct Epilogue {
+  static constexpr bool kFused = true;
+  static constexpr int kSmemBytes = 2 * 128 * 4;  // the bias of a tile's columns, one half per epilogue group
+  CUtensorMap map_r, map_z;  // residual and z: the boxes that D is stored in
+  const float* bias;
+  uint8_t* z8_codes;
+  uint8_t* z8_scales;
+  int z8_blocks;  // scale bytes of a row
+  int act, has_residual, has_z;
+};
+
+template <int ACT, int COLS>
+__device__ __forceinline__ void activate(uint32_t (&r)[COLS]) {
+#pragma unroll
+  for (int j = 0; j < COLS; ++j) r[j] = __float_as_uint(act_value<ACT>(__uint_as_float(r[j])));
+}
+
+// COLS columns of one row as a copy in 8 bits, straight from the registers: a thread has whole blocks, so their maxima need no
+// exchange, and the 32 bytes of a block are a sector.  Columns behind N are zeros in r.
+template <int COLS>
+__device__ __forceinline__ void store_row8(const uint32_t (&r)[COLS], const Epilogue& e, int64_t row, int x0, int N) {
+  uint32_t bytes = 0;
+  const bool wide = (N & 31) == 0 && (reinterpret_cast<uintptr_t>(e.z8_codes) & 31) == 0;
+  uint8_t* const scales = e.z8_scales + row * e.z8_blocks + (x0 >> 5);
+  const bool word = COLS == 128 && (e.z8_blocks & 3) == 0;
+#pragma unroll
+  for (int b = 0; b < COLS / 32; ++b) {
+    const int x = x0 + 32 * b;
+    if (x >= N) break;
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) m = amax3(m, __uint_as_float(r[32 * b + j]), __uint_as_float(r[32 * b + j + 1]));
+    const uint32_t byte = scale_byte8(m);
+    const float scale = encode_scale8(byte);
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t* const q = &r[32 * b + 4 * j];
+      w[j] = e4m3x4(__uint_as_float(q[0]) * scale, __uint_as_float(q[1]) * scale, __uint_as_float(q[2]) * scale, __uint_as_float(q[3]) * scale);
+    }
+    uint8_t* const dst = e.z8_codes + row * N + x;
+    if (wide) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                   : "memory");
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (x + 8 * j < N) *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(w[2 * j], w[2 * j + 1]);
+    }
+    if (word)
+      bytes |= byte << (8 * b);
+    else
+      scales[b] = (uint8_t)byte;
+  }
+  if (word && x0 < N) *reinterpret_cast<uint32_t*>(scales) = bytes;
+}
+
+// Units of 16 bytes of a staged row, as store_half() has them for bf16
+template <int COLS>
+constexpr int kStagedUnits = COLS < 64 ? 4 : 8;
+
+// The residual of the next chunk into the group's staging buffer, once the store before has read it (one thread)
+template <int COLS>
+__device__ __forceinline__ void load_residual(const Epilogue& e, uint32_t stage_buf, int x, int row0, uint32_t res_bar) {
+  pair::bulk_wait_read<0>();
+  mbar_expect_tx(res_bar, 128 * 16 * kStagedUnits<COLS>);
+  tma_load_2d(stage_buf, &e.map_r, x, row0, res_bar);
+}
+
+// The epilogue of COLS columns of one row per thread.  The residual comes by TMA into the staging buffer, in the place from which the
+// sum then leaves: a thread reads and writes its own row.  prefetched: the first chunk is on its way.  false: a wait ran out (all 128
+// threads agree).
+template <int COLS>
+__device__ __forceinline__ bool finish_half(uint32_t (&r)[COLS], const Epilogue& e, const float* bias, int M, int N, int et, int bar_id,
+                                            int row_in_tile, uint32_t stage_buf, const CUtensorMap* map_d, int x0, int row0,
+                                            uint32_t res_bar, uint32_t& res_phase, bool prefetched, volatile uint32_t* abort_flag) {
+  if (e.bias) {
+#pragma unroll
+    for (int j = 0; j < COLS; j += 4) {
+      const float4 b = *reinterpret_cast<const float4*>(bias + j);
+      r[j] = __float_as_uint(__uint_as_float(r[j]) + b.x);
+      r[j + 1] = __float_as_uint(__uint_as_float(r[j + 1]) + b.y);
+      r[j + 2] = __float_as_uint(__uint_as_float(r[j + 2]) + b.z);
+      r[j + 3] = __float_as_uint(__uint_as_float(r[j + 3]) + b.w);
+    }
+  }
+  if (e.z8_codes && row0 + row_in_tile < M) store_row8<COLS>(r, e, row0 + row_in_tile, x0, N);
+  if (e.has_z) pair::store_half<false, false, COLS>(r, 1.0f, et, bar_id, row_in_tile, stage_buf, &e.map_z, x0, row0, 0, false);
+  switch (e.act) {
+    case NVFP4_ACT_RELU2: activate<NVFP4_ACT_RELU2>(r); break;
+    case NVFP4_ACT_SILU: activate<NVFP4_ACT_SILU>(r); break;
+    case NVFP4_ACT_GELU: activate<NVFP4_ACT_GELU>(r); break;
+    default: break;
+  }
+  if (!e.has_residual) {
+    pair::store_half<false, false, COLS>(r, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, x0, row0, 0, false);
+    return true;
+  }
+  constexpr int kUnits = kStagedUnits<COLS>, kChunkCols = 8 * kUnits;
+#pragma unroll
+  for (int c = 0; c < COLS / kChunkCols; ++c) {
+    if (et == 0 && !(c == 0 && prefetched)) load_residual<COLS>(e, stage_buf, x0 + c * kChunkCols, row0, res_bar);
+    mbar_wait(res_bar, res_phase, abort_flag, 0xE00u);
+    res_phase ^= 1u;
+    if (group_gave_up(abort_flag, bar_id, 128)) return false;
+    const uint32_t srow = stage_buf + row_in_tile * (16 * kUnits);
+    const uint32_t x = kUnits == 4 ? (row_in_tile >> 1) & 3 : row_in_tile & 7;  // (the swizzles of store_half)
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      const uint32_t at = srow + ((j ^ x) << 4);
+      const uint4 w = pair::lds128(at);
+      const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+      uint32_t p[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        p[k] = pack2(__uint_as_float(r[c * kChunkCols + 8 * j + 2 * k]) + bf16_lo(in[k]),
+                     __uint_as_float(r[c * kChunkCols + 8 * j + 2 * k + 1]) + bf16_hi(in[k]));
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3]) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    asm volatile("bar.sync %0, 128;" ::"r"(bar_id) : "memory");
+    if (et == 0) {
+      pair::tma_store_2d(map_d, x0 + c * kChunkCols, row0, stage_buf);
+      pair::bulk_commit();
+    }
+  }
+  return true;
+}
+
 // kind::f16 instruction descriptor: FP32 accumulator (bit 4), BF16 x BF16 (format 1 at bits 7 and 10), operand
 // major-ness at bits 15 / 16 (0 = K-major), N >> 3 at bit 17, M >> 4 at bit 24
 __host__ __device__ constexpr uint32_t instr_desc_bf16(int m, int n, int a_mn, int b_mn) {
@@ -78,12 +215,14 @@ __device__ __forceinline__ void tc2_mma_bf16(uint32_t d_tmem, uint64_t adesc, ui
 // SPLIT > 1 (BN = 128): a cluster of SPLIT pairs takes one tile, the only one of its life,
 // each pair a share of the k-blocks (the exchange: pair::exchange_columns).
 // TWO: the launch has two problems.
-template <int BN, int SPLIT = 1, bool TWO = true>
+// E: Epilogue or NoEpilogue.
+template <int BN, int SPLIT = 1, bool TWO = true, class E = NoEpilogue>
 __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_bf16_pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
                           const __grid_constant__ CUtensorMap map_d0, const __grid_constant__ CUtensorMap map_a1,
                           const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_d1,
-                          const __grid_constant__ Args g) {
+                          const __grid_constant__ Args g, const __grid_constant__ E e) {
+  static_assert(!E::kFused || !TWO, "an epilogue belongs to one product");
   using namespace pair;
   constexpr int S = dense::Cfg<BN, SPLIT>::kStages, kStageBytes = dense::Cfg<BN, SPLIT>::kStageBytes;
   constexpr bool kDouble = BN == 512;        // two 256-column halves
@@ -99,6 +238,7 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
   auto acce_bar = [&](int b) { return bar_base + 8u * (2 * S + 2 + b); };  // leader only, 16 arrivals
   const uint32_t done_bar = bar_base + 8u * (2 * S + 4);
   const uint32_t recv_bar = done_bar + 16;                               // SPLIT > 1: all shares are here
+  auto res_bar = [&](int group) { return done_bar + 24u + 8u * group; };  // E: a chunk of the residual is here
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(
       base_ptr + S * kStageBytes + dense::kStagingBytes + 8 * (2 * S + 5));
   volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -163,6 +303,8 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     }
     mbar_init(done_bar, 2 * SPLIT - 1);
     if (SPLIT > 1) mbar_init(recv_bar, 1);
+    if (E::kFused)
+      for (int b = 0; b < 2; ++b) mbar_init(res_bar(b), 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -338,6 +480,9 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     const int row_in_tile = quad * 32 + lane;
     const uint32_t stage_buf = staging + half * 16384;
     int buf = 0, last_prob = 0, halves = 1;
+    [[maybe_unused]] uint32_t res_phase = 0;
+    [[maybe_unused]] float* const bias_s = reinterpret_cast<float*>(
+        base_ptr + S * kStageBytes + dense::kStagingBytes + 256 + dense::Cfg<BN, SPLIT>::kRecvBytes) + half * 128;
     // (kDouble: a tile comes up once for each of its halves, the second time without a step of the walk)
     for (int rnd = 0, half_no = 0, tile = pair_id; tile < n_tiles; tile = half_no ? tile : next_tile(++rnd)) {
       int prob, m_blk, n_blk;
@@ -352,6 +497,14 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
       const CUtensorMap* map_d = prob ? &map_d1 : &map_d0;
       const bool drain = prob != last_prob;  // the problems of a launch may have different output types
       last_prob = prob;
+      if constexpr (E::kFused) {  // what can be fetched while the tile's main loop runs
+        constexpr int kCols = SPLIT > 1 ? BN / SPLIT : HN / 2;  // columns that this group finishes (SPLIT > 1: if it finishes any)
+        const int x0 = SPLIT > 1 ? n_blk * BN + split * kCols : n_blk * HN + half * kCols;
+        // (the threads are behind the barriers of the tile before, and so behind their reads of its bias)
+        if (e.bias && et < kCols) bias_s[et] = x0 + et < g.p[0].N ? e.bias[x0 + et] : 0.f;
+        if (SPLIT == 1 && e.has_residual && !e.has_z && et == 0)
+          load_residual<kCols>(e, stage_buf, x0, m_blk * 256 + (int)rank * 128, res_bar(half));
+      }
       mbar_wait_cluster(accf_bar(buf), (acc_phase >> buf) & 1u, abort_flag, 0xC00u + buf);
       // agree on giving up: a warp that timed out still joins this barrier, and all 128 threads take ONE decision
       if (group_gave_up(abort_flag, bar_id, 128)) break;
@@ -372,10 +525,18 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
                                      abort_flag, bar_id))
           break;
         const int xs = n_blk * BN + split * kCols;
-        if (g.p[prob].d_is_fp32)
+        if constexpr (E::kFused) {
+          if (!finish_half<kCols>(v, e, bias_s, g.p[0].M, g.p[0].N, et, bar_id, row_in_tile, stage_buf, map_d, xs, row0, res_bar(half),
+                                  res_phase, false, abort_flag))
+            break;
+        } else if (g.p[prob].d_is_fp32)
           store_half<true, false, kCols>(v, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, xs, row0, g.p[prob].accumulate, drain);
         else
           store_half<false, false, kCols>(v, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, xs, row0, g.p[prob].accumulate, drain);
+      } else if constexpr (E::kFused) {
+        if (!finish_half<HN / 2>(r, e, bias_s, g.p[0].M, g.p[0].N, et, bar_id, row_in_tile, stage_buf, map_d, n_blk * HN + half * (HN / 2),
+                                 row0, res_bar(half), res_phase, !e.has_z, abort_flag))
+          break;
       } else if (g.p[prob].d_is_fp32)
         store_half<true, false, HN / 2>(r, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, n_blk * HN + half * (HN / 2),
                                         row0, g.p[prob].accumulate, drain);
