@@ -87,6 +87,9 @@ struct EpilogueArgs {
   int act;
 };
 cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& e, int tile, const Bf16Wide& wide, cudaStream_t s);
+// the same for at most kFewRows rows of A (gemm_few.cu)
+constexpr int kFewRows = 32;
+cudaError_t launch_gemm_few_rows(const DenseGemmArgs& g, const EpilogueArgs& e, cudaStream_t s);
 cudaError_t launch_gemm_bf16(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, const Bf16Wide& wide, cudaStream_t s);
 
 }  // namespace nvfp4

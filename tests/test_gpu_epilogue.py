@@ -22,8 +22,10 @@ def normal(shape, seed, std=1.0, dtype=torch.bfloat16):
     return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * std).to(dtype)
 
 
-# one CTA pair, few tiles with shared contractions, 128- and 256-wide tiles, several rounds, 512-wide tiles (rows off 32 bytes)
-SHAPES = [(1, 8, 8), (1, 136, 264), (3, 520, 72), (8, 256, 2048), (40, 264, 128), (129, 1000, 200), (257, 520, 1088), (300, 2056, 64),
+# few rows (up to 32: one to eight shares of k, short last blocks and steps); one CTA pair, few tiles with shared contractions, 128- and
+# 256-wide tiles, several rounds, 512-wide tiles (rows off 32 bytes)
+SHAPES = [(1, 8, 8), (1, 136, 264), (3, 520, 72), (8, 256, 2048), (9, 72, 520), (16, 2048, 4104), (17, 264, 16384), (31, 40, 40),
+          (32, 1048, 2056), (2, 20480, 264), (33, 1048, 2056), (40, 264, 128), (129, 1000, 200), (257, 520, 1088), (300, 2056, 64),
           (1000, 2504, 136), (2049, 2304, 72), (2305, 2600, 1032)]
 
 
@@ -81,7 +83,7 @@ def check(M, N, K, act, residual, keep, bias=True, std=1.0):
         R.assert_within(got, z64, off + np.maximum(2.0 ** -4 * (np.abs(z64) + off), 2.0 ** -10 * top / 224), "z8")
 
 
-@pytest.mark.parametrize("shape", [(1, 1024, 4096), (5, 264, 5120), (264, 512, 4096), (1000, 2000, 3000), (1040, 3664, 904), (4096, 1024, 256)])
+@pytest.mark.parametrize("shape", [(1, 1024, 4096), (5, 264, 5120), (12, 5128, 1032), (32, 136, 8200), (264, 512, 4096), (1000, 2000, 3000), (1040, 3664, 904), (4096, 1024, 256)])
 @pytest.mark.parametrize("act", sorted(R.ACTS))
 def test_random_data(shape, act):
     check(*shape, act, True, "bf16")
