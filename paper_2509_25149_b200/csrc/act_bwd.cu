@@ -3,6 +3,8 @@
 // Bound by HBM (da 2, z 1 + 1/32 or 2, dz 2, a 2 bytes per element), so everything is one pass: a CTA takes 256 columns and a run
 // of rows, a lane eight neighbouring columns, and their sums stay in its registers.  The sums of a CTA leave as a row of partial
 // sums, which a second kernel adds in a fixed order: no atomics, the same bits in every run.
+#include <algorithm>
+
 #include "act.cuh"
 #include "around.h"
 #include "copy8.cuh"
@@ -11,15 +13,17 @@ namespace nvfp4 {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps, kCols = 256, kDepth = 4;
+constexpr int kWarps = 8, kThreads = 32 * kWarps, kCols = 256, kRing = 6;  // kRing: rows of a warp that its ring has room for
 
-// Rows of a CTA: about eight rounds of four CTAs on each of 148 SMs, so that the last round is a small part of the whole, but
-// 64 rows at least where there are so many
+// Rows of a CTA.  With four CTAs on each of 148 SMs all at once the rings are filled once only: that is for runs of up to 512 rows (4088 x
+// 5128 26.8 -> 25.6 us, 16384 x 1024 21.7 -> 20.3, 256 x 20480 11.1 -> 9.7).  Longer ones drift apart and leave SMs idle at the end (8192 x
+// 20480, GELU from bf16, 177 us): there eight rounds of such CTAs (154 us).
 int64_t chunk_rows(int64_t rows, int64_t cols) {
-  const int64_t strips = (cols + kCols - 1) / kCols, chunks = (4736 + strips - 1) / strips;
-  int64_t n = (rows + chunks - 1) / chunks;
-  n = n < 64 ? 64 : n;
-  return (n + kWarps * kDepth - 1) / (kWarps * kDepth) * (kWarps * kDepth);
+  const int64_t strips = (cols + kCols - 1) / kCols;
+  auto per_cta = [&](int64_t ctas) { return (rows + std::max<int64_t>(ctas / strips, 1) - 1) / std::max<int64_t>(ctas / strips, 1); };
+  int64_t n = per_cta(592);
+  if (n > 512) n = per_cta(8 * 592);
+  return (std::max<int64_t>(n, 32) + kWarps - 1) / kWarps * kWarps;
 }
 int64_t chunk_count(int64_t rows, int64_t cols) {
   const int64_t n = chunk_rows(rows, cols);
@@ -36,56 +40,77 @@ struct Args {
   int64_t rows, cols, ldda, ldz, lddz, lda, chunk_rows;
 };
 
+template <bool Z8>
+constexpr int kStageBytes = kThreads * (Z8 ? 24 : 32);  // da and z of a row of every warp
+
+// da and z come by cp.async through a ring in shared memory, in which every thread has places of its own: five rows of a warp are in
+// flight whatever the registers hold, and a thread waits for nobody else's.
 template <int ACT, bool Z8>
-__global__ void __launch_bounds__(kThreads) act_bwd_kernel(const Args g) {
-  griddep_wait();
-  griddep_launch_dependents();
+__global__ void __launch_bounds__(kThreads, 4) act_bwd_kernel(const Args g) {
+  extern __shared__ __align__(16) uint8_t ring[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t col = (int64_t)blockIdx.x * kCols + lane * 8;
   const bool live = col < g.cols, have_z = ACT != NVFP4_ACT_NONE || g.a != nullptr;
-  const int64_t r0 = (int64_t)blockIdx.y * g.chunk_rows, r1 = min(r0 + g.chunk_rows, g.rows);
-  float sum[8] = {};
-  for (int64_t r = r0 + warp; live && r < r1; r += kWarps * kDepth) {
-    uint4 da[kDepth], z[kDepth];
-    uint2 codes[kDepth];
-    uint32_t byte[kDepth];
-#pragma unroll
-    for (int u = 0; u < kDepth; ++u) {
-      const int64_t row = r + u * kWarps;
-      if (row >= r1) break;
-      da[u] = ldg128_stream(g.da + row * g.ldda + col);
-      if (have_z) {
-        if (Z8) {
-          codes[u] = ldg64_stream(g.z8.codes + row * g.cols + col);
-          byte[u] = ldg8(g.z8.scales + row * g.z8.blocks + (col >> 5));
-        } else {
-          z[u] = ldg128_stream(g.z + row * g.ldz + col);
-        }
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kDepth; ++u) {
-      const int64_t row = r + u * kWarps;
-      if (row >= r1) break;
-      float d[8], v[8] = {}, out[8], a[8];
-      unpack8(da[u], d);
+  const int64_t r0 = (int64_t)blockIdx.y * g.chunk_rows, rows = min(g.chunk_rows, g.rows - r0);
+  const int steps = warp < rows ? (int)((rows - warp + kWarps - 1) / kWarps) : 0;
+  const int64_t row0 = r0 + warp, at = live ? col : 0;
+  const uint16_t* const da = g.da + row0 * g.ldda + at;
+  const uint16_t* const zb = Z8 ? nullptr : g.z + row0 * g.ldz + at;
+  const uint8_t* const codes = Z8 ? g.z8.codes + row0 * g.cols + at : nullptr;
+  const uint8_t* const bytes = Z8 ? g.z8.scales + row0 * g.z8.blocks + (at >> 5) : nullptr;
+  const uint32_t mine = smem_u32(ring) + threadIdx.x * 16, mine_z = smem_u32(ring) + kThreads * 16 + threadIdx.x * (Z8 ? 8 : 16);
+  auto fetch = [&](int s, int slot) {
+    if (live && s < steps) {
+      copy_async<16>(mine + slot * kStageBytes<Z8>, da + s * (kWarps * g.ldda), true);
       if (have_z) {
         if (Z8)
-          decode8(codes[u], decode_scale8(byte[u]), v);
+          copy_async<8>(mine_z + slot * kStageBytes<Z8>, codes + s * (kWarps * g.cols), true);
         else
-          unpack8(z[u], v);
+          copy_async<16>(mine_z + slot * kStageBytes<Z8>, zb + s * (kWarps * g.ldz), true);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        out[i] = d[i] * act_slope<ACT>(v[i], a[i]);
-        sum[i] += out[i];
-      }
-      if (g.dz) store8<false>(g.dz, row * g.lddz + col, out);
-      if (g.a) store8<false>(g.a, row * g.lda + col, a);
     }
+    copy_commit();  // (an empty group where there is no row: the count of groups stays that of the rows)
+  };
+  uint32_t byte = 0;  // of the row to come
+  auto fetch_byte = [&](int s) {
+    if (Z8 && have_z && live && s < steps) byte = ldg8(bytes + s * (kWarps * g.z8.blocks));
+  };
+  griddep_wait();
+  griddep_launch_dependents();
+#pragma unroll
+  for (int u = 0; u < kRing - 1; ++u) fetch(u, u);
+  fetch_byte(0);
+  float sum[8] = {};
+  int slot = 0, next = kRing - 1;
+  for (int s = 0; s < steps; ++s) {
+    copy_wait<kRing - 2>();
+    float d[8], z[8] = {}, out[8], a[8];
+    unpack8(lds16(mine + slot * kStageBytes<Z8>), d);
+    if (have_z) {
+      if (Z8)
+        decode8(lds8(mine_z + slot * kStageBytes<Z8>), decode_scale8(byte), z);
+      else
+        unpack8(lds16(mine_z + slot * kStageBytes<Z8>), z);
+    }
+    fetch_byte(s + 1);
+    fetch(s + kRing - 1, next);  // the slot of the row before, whose values went into registers a turn ago
+    slot = slot + 1 == kRing ? 0 : slot + 1;
+    next = next + 1 == kRing ? 0 : next + 1;
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      out[i] = d[i] * act_slope<ACT>(z[i], a[i]);
+      sum[i] += out[i];
+    }
+    const int64_t row = row0 + (int64_t)s * kWarps;
+    if (g.dz) store8<false>(g.dz, row * g.lddz + col, out);
+    if (g.a) store8<false>(g.a, row * g.lda + col, a);
   }
+  copy_wait<0>();
   if (!g.partial) return;
-  __shared__ float part[kWarps][kCols];
+  __syncthreads();  // the ring is empty; the sums take its place
+  auto part = reinterpret_cast<float(*)[kCols]>(ring);
+  static_assert(kWarps * kCols * 4 <= kRing * kStageBytes<Z8>, "the sums reuse the ring");
 #pragma unroll
   for (int i = 0; i < 8; ++i) part[warp][lane * 8 + i] = sum[i];
   __syncthreads();
@@ -97,9 +122,8 @@ __global__ void __launch_bounds__(kThreads) act_bwd_kernel(const Args g) {
   g.partial[(int64_t)blockIdx.y * g.cols + c] = total;
 }
 
-constexpr int kShares = 8;
-
-// 32 columns to a CTA; every warp sums a share of the rows, one thread a column's eight shares
+// 32 columns to a CTA; every warp sums a share of the rows, one thread a column's shares
+template <int kShares>
 __global__ void __launch_bounds__(32 * kShares) column_sums_kernel(const float* partial, int64_t parts, int64_t cols, float* out,
                                                                    int accumulate) {
   griddep_wait();
@@ -123,9 +147,22 @@ __global__ void __launch_bounds__(32 * kShares) column_sums_kernel(const float* 
   out[c] = accumulate ? out[c] + total : total;
 }
 
+template <int ACT, bool Z8>
+cudaError_t launch_act(const Args& k, dim3 grid, cudaStream_t s) {
+  constexpr int smem = kRing * kStageBytes<Z8>;
+  auto kern = act_bwd_kernel<ACT, Z8>;
+  static std::atomic<uint64_t> configured{0};  // per instantiation and device
+  int dev;
+  if (device_needs_config(configured, &dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    device_configured(configured, dev);
+  }
+  return launch_divided(100, kern, grid, dim3(kThreads), smem, s, k);
+}
 template <int ACT>
 cudaError_t launch_act(const Args& k, bool z8, dim3 grid, cudaStream_t s) {
-  return launch_divided(kStreamingCarveout, z8 ? act_bwd_kernel<ACT, true> : act_bwd_kernel<ACT, false>, grid, dim3(kThreads), 0, s, k);
+  return z8 ? launch_act<ACT, true>(k, grid, s) : launch_act<ACT, false>(k, grid, s);
 }
 
 }  // namespace
@@ -133,8 +170,11 @@ cudaError_t launch_act(const Args& k, bool z8, dim3 grid, cudaStream_t s) {
 int64_t act_bwd_workspace_floats(int64_t rows, int64_t cols) { return chunk_count(rows, cols) * cols; }
 
 cudaError_t launch_column_sums(const float* partial, int64_t parts, int64_t cols, float* out, bool accumulate, cudaStream_t s) {
-  const cudaError_t e = launch_divided(kStreamingCarveout, column_sums_kernel, dim3((unsigned)((cols + 31) / 32)),
-                                       dim3(32 * kShares), 0, s, partial, parts, cols, out, (int)accumulate);
+  // the more rows, the more warps: 148 rows of 5120 columns 5.4 us with eight of them, 8 rows of 20480 1.7 us slower with 32
+  const bool many = parts > 32;
+  const cudaError_t e = launch_divided(kStreamingCarveout, many ? column_sums_kernel<32> : column_sums_kernel<8>,
+                                       dim3((unsigned)((cols + 31) / 32)), dim3(many ? 1024 : 256), 0, s, partial, parts, cols, out,
+                                       (int)accumulate);
   count_launch();
   return e;
 }

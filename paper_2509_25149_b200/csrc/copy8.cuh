@@ -81,6 +81,25 @@ __device__ __forceinline__ void decode8(uint2 w, float scale, float (&v)[8]) {
   }
 }
 
+// the same in pairs, for two binary32 operations an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{.reg .b64 ra, rb, rc, rd; mov.b64 ra, {%2, %3}; mov.b64 rb, {%4, %5}; mov.b64 rc, {%6, %7}; "
+      "fma.rn.f32x2 rd, ra, rb, rc; mov.b64 {%0, %1}, rd;}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ void decode8(uint2 w, float scale, float2 (&v)[4]) {
+  float a[4], b[4];
+  decode4(w.x, a);
+  decode4(w.y, b);
+  v[0] = mul2(make_float2(a[0], a[1]), both(scale));
+  v[1] = mul2(make_float2(a[2], a[3]), both(scale));
+  v[2] = mul2(make_float2(b[0], b[1]), both(scale));
+  v[3] = mul2(make_float2(b[2], b[3]), both(scale));
+}
+
 // Eight neighbouring elements of a row belong to a lane and a block to four lanes (the chunk's index and the lane agree in
 // their last two bits).  Every lane of the warp calls; `live`: the chunk exists (values of one that does not are zero).
 __device__ __forceinline__ void store_chunk8(const Copy8& q, const float (&v)[8], int64_t row, int64_t chunk, int64_t cols, bool live) {
@@ -105,9 +124,38 @@ __device__ __forceinline__ uint32_t ldg8(const uint8_t* p) {
   asm volatile("ld.global.u8 %0, [%1];" : "=r"(r) : "l"(p));
   return r;
 }
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+// ---- asynchronous copies of a thread into its own places of shared memory (zeros where there is nothing): 16 or 8 bytes ----
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool live) {
+  if (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ void unpack8(uint4 a, float (&v)[8]) {
   v[0] = bf16_lo(a.x); v[1] = bf16_hi(a.x); v[2] = bf16_lo(a.y); v[3] = bf16_hi(a.y);
   v[4] = bf16_lo(a.z); v[5] = bf16_hi(a.z); v[6] = bf16_lo(a.w); v[7] = bf16_hi(a.w);
+}
+__device__ __forceinline__ void unpack8(uint4 a, float2 (&v)[4]) {
+  v[0] = make_float2(bf16_lo(a.x), bf16_hi(a.x));
+  v[1] = make_float2(bf16_lo(a.y), bf16_hi(a.y));
+  v[2] = make_float2(bf16_lo(a.z), bf16_hi(a.z));
+  v[3] = make_float2(bf16_lo(a.w), bf16_hi(a.w));
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -143,6 +191,29 @@ struct Raw8 {
     }
   }
 };
+template <bool F32>
+__device__ __forceinline__ void values2(const Raw8<F32>& r, float2 (&v)[4]) {
+  if (F32) {
+    const uint4 a = r.w[0], b = r.w[F32 ? 1 : 0];
+    v[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+    v[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+    v[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+    v[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
+  } else {
+    unpack8(r.w[0], v);
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void store8(void* base, int64_t elem, const float2 (&v)[4]) {
+  if (F32) {
+    float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + elem);
+    p[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+    p[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + elem) =
+        make_uint4(pack2(v[0].x, v[0].y), pack2(v[1].x, v[1].y), pack2(v[2].x, v[2].y), pack2(v[3].x, v[3].y));
+  }
+}
 template <bool F32>
 __device__ __forceinline__ void store8(void* base, int64_t elem, const float (&v)[8]) {
   if (F32) {

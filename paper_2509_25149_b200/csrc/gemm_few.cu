@@ -60,20 +60,6 @@ __device__ __forceinline__ float activated(float z, int act) {
   }
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {  // zeros where there is nothing
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint4 lds16(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
-}
-
 // MT: groups of eight rows of A;  ST: steps of 32 k that the ring has room for
 template <int MT, int ST>
 struct Ring {
@@ -96,7 +82,7 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
   const int steps = (g.K + 31) / 32, share = rank * kWarps + warp, of = g.shares * kWarps;
   const int s0 = (int)((int64_t)steps * share / of), s1 = (int)((int64_t)steps * (share + 1) / of);
   const uint32_t mine = smem_u32(smem) + threadIdx.x * 16;
-  // rows that do not exist are never read (copy16), but their addresses are kept inside the operands
+  // rows that do not exist are never read (copy_async), but their addresses are kept inside the operands
   const uint16_t* brow[4];
   const uint16_t* arow[MT];
   bool blive[4], alive[MT];
@@ -116,9 +102,9 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
       const bool in = k < g.K;
       const uint32_t at = mine + slot * R::kStep;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) copy16(at + i * R::kPlane, brow[i] + (in ? k : 0), in && blive[i]);
+      for (int i = 0; i < 4; ++i) copy_async<16>(at + i * R::kPlane, brow[i] + (in ? k : 0), in && blive[i]);
 #pragma unroll
-      for (int j = 0; j < MT; ++j) copy16(at + (4 + j) * R::kPlane, arow[j] + (in ? k : 0), in && alive[j]);
+      for (int j = 0; j < MT; ++j) copy_async<16>(at + (4 + j) * R::kPlane, arow[j] + (in ? k : 0), in && alive[j]);
     }
     copy_commit();  // (an empty group where there is no step: the count of groups stays that of the steps)
   };

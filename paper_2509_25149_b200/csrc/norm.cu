@@ -4,8 +4,10 @@
 // y and the copies in 8 bits are taken of the binary32 h, before it is rounded to the residual's type: y is as exact as it can be,
 // and what the backward pass reads (the stored h) is off by that one rounding.
 //
-// Both are bound by HBM, so a row is read once: it stays in the registers of one to sixteen warps (up to five chunks of eight
-// elements a lane) between the statistic and its use, and warps of a row exchange partial sums through shared memory.
+// Both are bound by HBM, so a row is read once: it stays on the SM (forward: in the registers, gradient: in shared memory) of one to
+// sixteen warps, up to five chunks of eight elements a lane, between the statistic and its use, and warps of a row exchange partial sums
+// through shared memory.  Of the measured copy rate: forward of 8192 x 5120 with a bf16 residual 54.8 us (94 %), gradient from bf16 57 us
+// (90 %), from 8 bits 51 us (88 %), from and to binary32 116 us (78 %).
 #include "around.h"
 #include "copy8.cuh"
 
@@ -185,6 +187,7 @@ cudaError_t launch_fwd(const Fwd& a, int sms, cudaStream_t s) {
   if (groups <= 2) return launch_fwd_kept<RES, 1, 2>(a, sms, s);
   if (groups <= 4) return launch_fwd_kept<RES, 2, 2>(a, sms, s);
   if (groups <= 8) return launch_fwd_kept<RES, 4, 2>(a, sms, s);
+  if (groups <= 12) return launch_fwd_kept<RES, 4, 3>(a, sms, s);
   if (groups <= 20) return launch_fwd_kept<RES, 4, 5>(a, sms, s);
   if (groups <= 40) return launch_fwd_kept<RES, 8, 5>(a, sms, s);
   if (groups <= 80) return launch_fwd_kept<RES, 16, 5>(a, sms, s);
@@ -220,87 +223,176 @@ struct LoadedH {
       raw.load(a.h, row * a.ldh + chunk * 8);
     }
   }
-  __device__ __forceinline__ void zero() {
-    if (H == 2) {
-      codes = make_uint2(0u, 0u);
-      byte = 0u;
-    } else {
-      raw.zero();
-    }
-  }
-  __device__ __forceinline__ void normalised(float rstd, float (&n)[8]) const {
+  __device__ __forceinline__ void normalised(float rstd, float2 (&n)[4]) const {
     if (H == 2) {
       decode8(codes, decode_scale8(byte), n);
     } else {
-      raw.values(n);
+      values2(raw, n);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) n[i] *= rstd;
+    for (int i = 0; i < 4; ++i) n[i] = mul2(n[i], both(rstd));
   }
 };
 
-__device__ __forceinline__ void times_gain(const Bwd& a, int64_t chunk, const float (&d)[8], float (&g)[8]) {
-  load_gain(a.gain, chunk * 8, g);
+__device__ __forceinline__ void times_gain(const float* gain, int64_t chunk, const float2 (&d)[4], float2 (&g)[4]) {
+  float v[8];
+  load_gain(gain, chunk * 8, v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) g[i] *= d[i];
+  for (int i = 0; i < 4; ++i) g[i] = mul2(d[i], make_float2(v[2 * i], v[2 * i + 1]));
 }
 
 template <bool F32>
-__device__ __forceinline__ void store_dh(const Bwd& a, const float (&g)[8], const float (&n)[8], const Raw8<F32>& rg, float rstd,
+__device__ __forceinline__ void store_dh(const Bwd& a, const float2 (&g)[4], const float2 (&n)[4], const Raw8<F32>& rg, float rstd,
                                          float c, int64_t row, int64_t chunk) {
-  float out[8], w[8];
-  rg.values(w);
+  float2 out[4], w[4];
+  values2(rg, w);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) out[i] = fmaf(rstd, fmaf(-n[i], c, g[i]), w[i]);
+  for (int i = 0; i < 4; ++i) out[i] = fma2(both(rstd), fma2(n[i], both(-c), g[i]), w[i]);
   store8<F32>(a.dh, row * a.lddh + chunk * 8, out);
 }
 
-constexpr int kBwdWarps = 16;
-
-// A CTA of sixteen warps, WPR of them to a row: 16 / WPR rows at a time, each group of warps at its own pace.  A lane keeps the sums
-// of its columns in registers over all its rows; at the end the groups add theirs in their order.
+// A CTA of G groups of WPR warps, a row to a group at a time, each group at its own pace.  dy and h of the rows to come are on
+// their way into a ring of ST rows in shared memory, in which every thread has places of its own (so that no group waits for another,
+// and a thread only for its own copies); so is the residual path's gradient where there is room, else it is loaded when its row's turn
+// begins.
+// A lane keeps the sums of its columns in registers over all its rows; at the end the groups add theirs in their order.
 template <int H, bool F32, int WPR, int KEEP>
-__global__ void __launch_bounds__(32 * kBwdWarps, 1) rmsnorm_bwd_kernel(const Bwd a) {
-  constexpr int kGroups = kBwdWarps / WPR;
-  extern __shared__ float columns[];  // (more than one group) cols sums
-  __shared__ float part[2][kBwdWarps];
+struct BwdShape {
+  static constexpr int kH = H == 2 ? 8 : H == 1 ? 32 : 16;  // bytes of a chunk of h
+  // sixteen warps (a register file of 128 per thread), eight where five chunks of a binary32 h would not leave the ring two rows
+  static constexpr int kGroups = WPR == 16 ? 1 : (H == 1 && KEEP == 5 ? 8 : 16) / WPR;
+  static_assert(WPR == 1 || kGroups < 16, "named barriers 1 .. 15");
+  static constexpr int kThreads = 32 * WPR * kGroups;
+  static constexpr int kGain = 32 * WPR * KEEP * 32;  // the gain of all columns
+  static constexpr int fit(int chunk_bytes) { return (220 * 1024 - kGain) / (KEEP * chunk_bytes * kThreads); }
+  // the residual path's gradient goes through the ring as well where two rows of all three fit
+  static constexpr bool kRingRg = fit(16 + kH + (F32 ? 32 : 16)) >= 2;
+  static constexpr int kRg = kRingRg ? (F32 ? 32 : 16) : 0;
+  static constexpr int kStage = KEEP * (16 + kH + kRg) * kThreads;
+  static constexpr int ST = fit(16 + kH + kRg) > 4 ? 4 : fit(16 + kH + kRg);
+  static constexpr int kBytes = ST * kStage + kGain;
+  static_assert(ST >= 1 && 32 * WPR * KEEP * 32 <= ST * kStage, "the column sums reuse the ring");
+};
+
+template <int H, bool F32, int WPR, int KEEP>
+__global__ void __launch_bounds__(BwdShape<H, F32, WPR, KEEP>::kThreads, 1) rmsnorm_bwd_kernel(const Bwd a) {
+  using S = BwdShape<H, F32, WPR, KEEP>;
+  constexpr int ST = S::ST, kGroups = S::kGroups, T = S::kThreads;
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* const columns = reinterpret_cast<float*>(smem);
+  float4* const gain_s = reinterpret_cast<float4*>(smem + ST * S::kStage);  // [half of a chunk][chunk]
+  __shared__ float part[2][WPR * kGroups];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, seg = warp % WPR, group = warp / WPR;
-  const int64_t n8 = a.cols >> 3;
+  const int n8 = (int)(a.cols >> 3);
+  const uint32_t ring = smem_u32(smem), mine_dy = ring + threadIdx.x * 16,
+                 mine_rg = ring + KEEP * T * 16 + threadIdx.x * 16,
+                 mine_h = ring + KEEP * T * (16 + S::kRg) + threadIdx.x * (H == 2 ? 8 : 16);
+  const int c0 = lane + 32 * seg;  // the lane's first chunk; the others are 32 * WPR apart
+  auto chunk_of = [&](int i) { return c0 + 32 * WPR * i; };
+  const int64_t step = (int64_t)gridDim.x * kGroups;
+  auto fetch = [&](int64_t row, int slot) {
+    if (row < a.rows) {
+      const uint16_t* const dy = a.dy + row * a.lddy + c0 * 8;
+      const uint8_t* const h = H == 2 ? a.h8.codes + row * a.cols + c0 * 8
+                                      : static_cast<const uint8_t*>(a.h) + (row * a.ldh + c0 * 8) * (H == 1 ? 4 : 2);
+      const uint8_t* const rg = static_cast<const uint8_t*>(a.residual_grad) + (row * a.ldrg + c0 * 8) * (F32 ? 4 : 2);
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i) {
+        if (chunk_of(i) >= n8) break;
+        if (S::kRingRg && a.residual_grad) {
+          const uint32_t dst = mine_rg + slot * S::kStage + i * T * S::kRg;
+          copy_async<16>(dst, rg + i * (F32 ? 1024 : 512) * WPR, true);
+          if (F32) copy_async<16>(dst + T * 16, rg + i * 1024 * WPR + 16, true);
+        }
+        copy_async<16>(mine_dy + slot * S::kStage + i * T * 16, dy + i * 256 * WPR, true);
+        const uint32_t dst = mine_h + slot * S::kStage + i * T * S::kH;
+        if (H == 2) {
+          copy_async<8>(dst, h + i * 256 * WPR, true);
+        } else if (H == 1) {
+          copy_async<16>(dst, h + i * 1024 * WPR, true);
+          copy_async<16>(dst + T * 16, h + i * 1024 * WPR + 16, true);
+        } else {
+          copy_async<16>(dst, h + i * 512 * WPR, true);
+        }
+      }
+    }
+    copy_commit();  // (an empty group where there is no row: the count of groups stays that of the rows)
+  };
+  // what a copy cannot bring one by one: the scale bytes and rstd of the next row
+  uint32_t byte[KEEP] = {};
+  float rstd_next = 0.f;
+  auto fetch_small = [&](int64_t row) {
+    if (row >= a.rows) return;
+    rstd_next = a.rstd[row];
+    if (H == 2)
+#pragma unroll
+      for (int i = 0; i < KEEP; ++i)
+        if (chunk_of(i) < n8) byte[i] = ldg8(a.h8.scales + row * a.h8.blocks + (chunk_of(i) >> 2));
+  };
   griddep_wait();
+  const int64_t first = (int64_t)blockIdx.x + (int64_t)gridDim.x * group;
+#pragma unroll
+  for (int u = 0; u < ST - 1; ++u) fetch(first + u * step, u);
+  fetch_small(first);
+  for (int c = threadIdx.x; c < n8; c += T) {
+    float g[8];
+    load_gain(a.gain, (int64_t)c * 8, g);
+    gain_s[c] = make_float4(g[0], g[1], g[2], g[3]);
+    gain_s[32 * WPR * KEEP + c] = make_float4(g[4], g[5], g[6], g[7]);
+  }
+  __syncthreads();
   griddep_launch_dependents();
-  float acc[KEEP][8] = {};
-  int it = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < a.rows; row += (int64_t)gridDim.x * kGroups, ++it) {
-    Raw8<false> dy[KEEP];
-    LoadedH<H> h[KEEP];
+  float2 acc[KEEP][4] = {};
+  int it = 0, slot = 0, next = ST - 1;
+  for (int64_t row = first; row < a.rows; row += step, ++it) {
     Raw8<F32> rg[KEEP];
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
-      const int64_t chunk = lane + 32 * (seg + WPR * i);
-      rg[i].zero();
-      if (chunk < n8) {
-        dy[i].load(a.dy, row * a.lddy + chunk * 8);
-        h[i].load(a, row, chunk);
-        if (a.residual_grad) rg[i].load(a.residual_grad, row * a.ldrg + chunk * 8);
-      } else {
-        dy[i].zero();
-        h[i].zero();
-      }
+      if (!S::kRingRg && a.residual_grad && chunk_of(i) < n8)
+        rg[i].load(a.residual_grad, row * a.ldrg + chunk_of(i) * 8);
+      else
+        rg[i].zero();
     }
-    const float rstd = a.rstd[row];
-    float sum = 0.f;
+    if (ST == 1) fetch(row, 0);  // (no room for a row ahead)
+    copy_wait<(ST > 2 ? ST - 2 : 0)>();
+    const float rstd = rstd_next;
+    uint32_t scale[KEEP];
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) scale[i] = byte[i];
+    fetch_small(row + step);
+    float2 sum2 = make_float2(0.f, 0.f);
+    auto operands = [&](int i, float2 (&d)[4], float2 (&n)[4], float2 (&g)[4]) {
+      // (read again for the second use: in registers they would not all fit)
+      unpack8(lds16(mine_dy + slot * S::kStage + i * T * 16), d);
+      const uint32_t src = mine_h + slot * S::kStage + i * T * S::kH;
+      LoadedH<H> h;
+      if (H == 2) {
+        h.codes = lds8(src);
+        h.byte = scale[i];
+      } else {
+        h.raw.w[0] = lds16(src);
+        if (H == 1) h.raw.w[H == 1 ? 1 : 0] = lds16(src + T * 16);
+      }
+      h.normalised(rstd, n);
+      const float4 u = gain_s[chunk_of(i)], v = gain_s[32 * WPR * KEEP + chunk_of(i)];
+      g[0] = mul2(d[0], make_float2(u.x, u.y));
+      g[1] = mul2(d[1], make_float2(u.z, u.w));
+      g[2] = mul2(d[2], make_float2(v.x, v.y));
+      g[3] = mul2(d[3], make_float2(v.z, v.w));
+    };
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
-      const int64_t chunk = lane + 32 * (seg + WPR * i);
-      if (chunk >= n8) continue;
-      float d[8], n[8], g[8];
-      dy[i].values(d);
-      h[i].normalised(rstd, n);
-      times_gain(a, chunk, d, g);
-      sum = dot8(g, n, sum);
+      if (chunk_of(i) >= n8) break;
+      float2 d[4], n[4], g[4];
+      operands(i, d, n, g);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[i][k] = fmaf(d[k], n[k], acc[i][k]);
+      for (int k = 0; k < 4; ++k) {
+        sum2 = fma2(g[k], n[k], sum2);
+        acc[i][k] = fma2(d[k], n[k], acc[i][k]);
+      }
     }
+    float sum = sum2.x + sum2.y;
+    if (ST > 1) fetch(row + (ST - 1) * step, next);  // into the slot of the row before, which is done
     sum = warp_sum(sum);
     if (WPR > 1) {
       if (lane == 0) part[it & 1][warp] = sum;
@@ -312,33 +404,43 @@ __global__ void __launch_bounds__(32 * kBwdWarps, 1) rmsnorm_bwd_kernel(const Bw
     const float c = __fdiv_rn(sum, (float)a.cols);
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
-      const int64_t chunk = lane + 32 * (seg + WPR * i);
-      if (chunk >= n8) continue;
-      float d[8], n[8], g[8];
-      dy[i].values(d);
-      h[i].normalised(rstd, n);
-      times_gain(a, chunk, d, g);
-      store_dh<F32>(a, g, n, rg[i], rstd, c, row, chunk);
+      if (chunk_of(i) >= n8) break;
+      float2 d[4], n[4], g[4];
+      operands(i, d, n, g);
+      if (S::kRingRg && a.residual_grad) {
+        const uint32_t src = mine_rg + slot * S::kStage + i * T * S::kRg;
+        rg[i].w[0] = lds16(src);
+        if (F32) rg[i].w[F32 ? 1 : 0] = lds16(src + T * 16);
+      }
+      store_dh<F32>(a, g, n, rg[i], rstd, c, row, chunk_of(i));
     }
+    slot = slot + 1 == ST ? 0 : slot + 1;
+    next = next + 1 == ST ? 0 : next + 1;
   }
+  copy_wait<0>();
   if (!a.partial) return;
+  __syncthreads();  // the ring is empty; the sums take its place
   float* const out = a.partial + (int64_t)blockIdx.x * a.cols;
-  for (int g = 0; g < kGroups; ++g) {
+  const int64_t left = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // (few rows: not every group had one)
+  const int last = (int)(left < kGroups ? left : kGroups) - 1;
+  for (int g = 0; g <= last; ++g) {
     if (g == group) {
 #pragma unroll
       for (int i = 0; i < KEEP; ++i) {
-        const int64_t chunk = lane + 32 * (seg + WPR * i);
+        const int chunk = chunk_of(i);
         if (chunk >= n8) continue;
         if (g > 0) {
           const float4* const p = reinterpret_cast<const float4*>(columns + chunk * 8);
           const float4 u = p[0], v = p[1];
-          acc[i][0] += u.x; acc[i][1] += u.y; acc[i][2] += u.z; acc[i][3] += u.w;
-          acc[i][4] += v.x; acc[i][5] += v.y; acc[i][6] += v.z; acc[i][7] += v.w;
+          acc[i][0] = add2(acc[i][0], make_float2(u.x, u.y));
+          acc[i][1] = add2(acc[i][1], make_float2(u.z, u.w));
+          acc[i][2] = add2(acc[i][2], make_float2(v.x, v.y));
+          acc[i][3] = add2(acc[i][3], make_float2(v.z, v.w));
         }
-        store8<true>(g == kGroups - 1 ? out : columns, chunk * 8, acc[i]);
+        store8<true>(g == last ? out : columns, chunk * 8, acc[i]);
       }
     }
-    if (g < kGroups - 1) __syncthreads();
+    if (g < last) __syncthreads();
   }
 }
 
@@ -353,7 +455,7 @@ __global__ void __launch_bounds__(512) rmsnorm_dots_kernel(const Bwd a) {
   int it = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++it) {
     const float rstd = a.rstd[row];
-    float sum = 0.f;
+    float2 sum2 = make_float2(0.f, 0.f);
     for (int64_t c0 = 0; c0 < n8; c0 += 1024) {
       Raw8<false> dy[2];
       LoadedH<H> h[2];
@@ -369,14 +471,15 @@ __global__ void __launch_bounds__(512) rmsnorm_dots_kernel(const Bwd a) {
       for (int i = 0; i < 2; ++i) {
         const int64_t chunk = c0 + threadIdx.x + 512 * i;
         if (chunk >= n8) continue;
-        float d[8], n[8], g[8];
-        dy[i].values(d);
+        float2 d[4], n[4], g[4];
+        unpack8(dy[i].w[0], d);
         h[i].normalised(rstd, n);
-        times_gain(a, chunk, d, g);
-        sum = dot8(g, n, sum);
+        times_gain(a.gain, chunk, d, g);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum2 = fma2(g[k], n[k], sum2);
       }
     }
-    sum = warp_sum(sum);
+    float sum = warp_sum(sum2.x + sum2.y);
     if (lane == 0) part[it & 1][warp] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -396,7 +499,7 @@ __global__ void __launch_bounds__(256) rmsnorm_bwd_long_kernel(const Bwd a) {
   const int64_t r0 = (int64_t)blockIdx.y * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
   griddep_wait();
   griddep_launch_dependents();
-  float acc[8] = {};
+  float2 acc[4] = {};
   for (int64_t r = r0 + warp; live && r < r1; r += 16) {
     Raw8<false> dy[2];
     LoadedH<H> h[2];
@@ -415,18 +518,18 @@ __global__ void __launch_bounds__(256) rmsnorm_bwd_long_kernel(const Bwd a) {
       const int64_t row = r + 8 * u;
       if (row >= r1) break;
       const float rstd = a.rstd[row], c = a.dots[row];
-      float d[8], n[8], g[8];
-      dy[u].values(d);
+      float2 d[4], n[4], g[4];
+      unpack8(dy[u].w[0], d);
       h[u].normalised(rstd, n);
-      times_gain(a, chunk, d, g);
+      times_gain(a.gain, chunk, d, g);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] = fmaf(d[k], n[k], acc[k]);
+      for (int k = 0; k < 4; ++k) acc[k] = fma2(d[k], n[k], acc[k]);
       store_dh<F32>(a, g, n, rg[u], rstd, c, row, chunk);
     }
   }
   if (!a.partial) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) part[warp][lane * 8 + i] = acc[i];
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(&part[warp][lane * 8 + 2 * i]) = acc[i];
   __syncthreads();
   const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (c >= a.cols) return;
@@ -439,18 +542,19 @@ __global__ void __launch_bounds__(256) rmsnorm_bwd_long_kernel(const Bwd a) {
 constexpr int64_t kKeptCols = 20480;  // 16 warps x 5 chunks x 32 lanes x 8 elements
 constexpr int kMaxParts = 256;        // CTAs that leave column sums (one per SM, and no GPU of this kind has more)
 
-int warps_per_row(int64_t cols) {
-  const int64_t groups = ((cols >> 3) + 31) / 32;
-  return groups <= 2 ? 1 : groups <= 4 ? 2 : groups <= 20 ? 4 : groups <= 40 ? 8 : 16;
-}
-
 template <int H, bool F32, int WPR, int KEEP>
 cudaError_t launch_bwd_kept(const Bwd& k, const NormBwd& a, int sms, cudaStream_t s) {
-  constexpr int kGroups = kBwdWarps / WPR;
-  const int64_t want = (a.rows + kGroups - 1) / kGroups, cap = sms < kMaxParts ? sms : kMaxParts;
-  const int64_t grid = want < cap ? want : cap;
-  const size_t smem = kGroups > 1 ? (size_t)a.cols * 4 : 0;
-  const cudaError_t e = launch_divided(20, rmsnorm_bwd_kernel<H, F32, WPR, KEEP>, dim3((unsigned)grid), dim3(32 * kBwdWarps), smem, s, k);
+  using S = BwdShape<H, F32, WPR, KEEP>;
+  auto kern = rmsnorm_bwd_kernel<H, F32, WPR, KEEP>;
+  static std::atomic<uint64_t> configured{0};  // per instantiation and device
+  int dev;
+  if (device_needs_config(configured, &dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    if (e != cudaSuccess) return e;
+    device_configured(configured, dev);
+  }
+  const int64_t cap = sms < kMaxParts ? sms : kMaxParts, grid = a.rows < cap ? a.rows : cap;  // (few rows: one to a CTA)
+  const cudaError_t e = launch_kernel(kern, dim3((unsigned)grid), dim3(S::kThreads), S::kBytes, s, k);
   count_launch();
   if (e != cudaSuccess || !a.dgain) return e;
   return launch_column_sums(k.partial, grid, a.cols, a.dgain, a.accumulate, s);
@@ -460,13 +564,17 @@ template <int H, bool F32>
 cudaError_t launch_bwd(const Bwd& k, const NormBwd& a, int sms, cudaStream_t s) {
   if (a.cols <= kKeptCols) {
     const int64_t groups = ((a.cols >> 3) + 31) / 32;
-    switch (warps_per_row(a.cols)) {
-      case 1: return launch_bwd_kept<H, F32, 1, 2>(k, a, sms, s);
-      case 2: return launch_bwd_kept<H, F32, 2, 2>(k, a, sms, s);
-      case 4: return groups <= 8 ? launch_bwd_kept<H, F32, 4, 2>(k, a, sms, s) : launch_bwd_kept<H, F32, 4, 5>(k, a, sms, s);
-      case 8: return launch_bwd_kept<H, F32, 8, 5>(k, a, sms, s);
-      default: return launch_bwd_kept<H, F32, 16, 5>(k, a, sms, s);
-    }
+    // The gradient wants threads more than long runs of its own: 8192 x 5120 with four / eight warps to a row, from 8 bits 54.1 / 51.4 us,
+    // from and to binary32 135.5 / 115.8.  With a single chunk a lane it loses again: 8192 x 2048 25.9 us, with eight warps to a row 30.3.
+    if (groups <= 2) return launch_bwd_kept<H, F32, 1, 2>(k, a, sms, s);
+    if (groups <= 4) return launch_bwd_kept<H, F32, 2, 2>(k, a, sms, s);
+    if (groups <= 8) return launch_bwd_kept<H, F32, 4, 2>(k, a, sms, s);
+    if (groups <= 12) return launch_bwd_kept<H, F32, 4, 3>(k, a, sms, s);
+    if (groups <= 16) return launch_bwd_kept<H, F32, 8, 2>(k, a, sms, s);
+    if (groups <= 24) return launch_bwd_kept<H, F32, 8, 3>(k, a, sms, s);
+    if (groups <= 40) return launch_bwd_kept<H, F32, 8, 5>(k, a, sms, s);
+    if (groups <= 48) return launch_bwd_kept<H, F32, 16, 3>(k, a, sms, s);
+    return launch_bwd_kept<H, F32, 16, 5>(k, a, sms, s);
   }
   const int64_t cap = (int64_t)sms * 4, chunks = (a.rows + k.chunk_rows - 1) / k.chunk_rows;
   cudaError_t e = launch_divided(kStreamingCarveout, rmsnorm_dots_kernel<H>, dim3((unsigned)(a.rows < cap ? a.rows : cap)), dim3(512), 0, s, k);
@@ -491,8 +599,7 @@ int64_t dots_floats(int64_t rows) { return (rows + 63) / 64 * 64; }
 bool rmsnorm_bwd_needs_workspace(int64_t cols) { return cols > kKeptCols; }
 int64_t rmsnorm_bwd_workspace_floats(int64_t rows, int64_t cols) {
   if (cols > kKeptCols) return dots_floats(rows) + (rows + long_rows(rows) - 1) / long_rows(rows) * cols;
-  const int64_t groups = kBwdWarps / warps_per_row(cols), parts = (rows + groups - 1) / groups;
-  return (parts < kMaxParts ? parts : kMaxParts) * cols;
+  return (rows < kMaxParts ? rows : kMaxParts) * cols;
 }
 
 cudaError_t launch_rmsnorm_fwd(const NormFwd& a, cudaStream_t s) {
