@@ -345,28 +345,50 @@ def nvfp4_dequantize(t: NVFP4Tensor, out: Optional[torch.Tensor] = None) -> torc
 
 
 # ---- around the linear layers -------------------------------------------------------------------------------------------
-_BF16_OR_FP32 = (torch.bfloat16, torch.float32)
+_BF16, _BF16_OR_FP32 = (torch.bfloat16,), (torch.bfloat16, torch.float32)
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, *dtypes) -> int:
-    """Checks a row-major matrix and returns its leading dimension."""
-    assert t.is_cuda and t.dtype in dtypes and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols
-    assert t.stride(1) == 1
-    return t.stride(0) if rows > 1 else cols  # (a single row's stride says nothing)
+def _device() -> int:
+    """The current device, which the calls launch on."""
+    return _get_device() if _get_device is not None else torch.cuda.current_device()
 
 
-def _vector(t: Optional[torch.Tensor], n: int) -> Optional[int]:
+def _matrix(t: torch.Tensor, shape, device: int, dtypes=_BF16) -> int:
+    """Checks a row-major matrix on the current device and returns its leading dimension."""
+    stride = t.stride()
+    assert t.get_device() == device and t.dtype in dtypes and t.shape == shape and len(stride) == 2 and stride[1] == 1, \
+        f"a row-major {tuple(shape)} matrix of {dtypes} on the current device is wanted, not {tuple(t.shape)} {t.dtype} on {t.device}"
+    return stride[0] if shape[0] > 1 else shape[1]  # (a single row's stride says nothing)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == torch.float32 and t.dim() == 1 and t.shape[0] == n and (n == 1 or t.stride(0) == 1)
+    assert t.get_device() == device and t.dtype == torch.float32 and t.shape == (n,) and (n == 1 or t.stride(0) == 1), \
+        f"a binary32 vector of {n} on the current device is wanted, not {tuple(t.shape)} {t.dtype} on {t.device}"
     return t.data_ptr()
+
+
+def _copy8(t: NVFP4Tensor, device: int) -> bytes:
+    assert t.codes.get_device() == device and t.scales.get_device() == device, "a copy on the current device is wanted"
+    assert t.codes.numel() >= t.rows * t.cols and t.scales.numel() >= t.rows * ((t.cols + 31) // 32)
+    return _TENSOR_FIELDS.pack(t.codes.data_ptr(), t.scales.data_ptr(), 0, t.rows, t.cols, t.sf_layout, t.format)
+
+
+def _scratch(t: Optional[torch.Tensor], device: int):
+    """Address and size of a workspace."""
+    if t is None:
+        return None, 0
+    assert t.get_device() == device and t.is_contiguous()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def nvfp4_dequantize_bf16(t: NVFP4Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values of an MXFP8 copy in bf16."""
     if out is None:
         out = torch.empty((t.rows, t.cols), dtype=torch.bfloat16, device=t.codes.device)
-    _check(lib().nvfp4_dequantize_bf16(t.packed(), out.data_ptr(), _matrix(out, t.rows, t.cols, torch.bfloat16), _stream()),
+    dev = _device()
+    _check(lib().nvfp4_dequantize_bf16(_copy8(t, dev), out.data_ptr(), _matrix(out, (t.rows, t.cols), dev), _stream()),
            "nvfp4_dequantize_bf16")
     return out
 
@@ -376,15 +398,20 @@ def nvfp4_rmsnorm_fwd(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
                       h: Optional[torch.Tensor] = None, y8: Optional[NVFP4Tensor] = None,
                       h8: Optional[NVFP4Tensor] = None) -> None:
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gain; y8, h8: MXFP8 copies of y and h."""
-    rows, cols = x.shape
-    fp32 = residual is not None and residual.dtype == torch.float32
-    assert h is None or residual is None or h.dtype == residual.dtype
-    _check(lib().nvfp4_rmsnorm_fwd(
-        x.data_ptr(), _matrix(x, rows, cols, torch.bfloat16), _ptr(residual),
-        _matrix(residual, rows, cols, *_BF16_OR_FP32) if residual is not None else 0, fp32, _vector(gain, cols), rows, cols, eps,
-        _ptr(h), _matrix(h, rows, cols, *_BF16_OR_FP32) if h is not None else 0,
-        _ptr(y), _matrix(y, rows, cols, torch.bfloat16) if y is not None else 0, _ref(y8), _ref(h8), _vector(rstd, rows), _stream()),
-        "nvfp4_rmsnorm_fwd")
+    dev, shape = _device(), x.shape
+    rows, cols = shape
+    ldx = _matrix(x, shape, dev)
+    pr = ldr = fp32 = ph = ldh = py = ldy = 0
+    if residual is not None:
+        pr, ldr, fp32 = residual.data_ptr(), _matrix(residual, shape, dev, _BF16_OR_FP32), residual.dtype == torch.float32
+    if h is not None:
+        assert residual is None or h.dtype == residual.dtype
+        ph, ldh = h.data_ptr(), _matrix(h, shape, dev, _BF16_OR_FP32)
+    if y is not None:
+        py, ldy = y.data_ptr(), _matrix(y, shape, dev)
+    _check(lib().nvfp4_rmsnorm_fwd(x.data_ptr(), ldx, pr, ldr, fp32, _vector(gain, cols, dev), rows, cols, eps, ph, ldh, py, ldy,
+                                   _copy8(y8, dev) if y8 is not None else None, _copy8(h8, dev) if h8 is not None else None,
+                                   _vector(rstd, rows, dev), _stream()), "nvfp4_rmsnorm_fwd")
 
 
 def nvfp4_rmsnorm_bwd_workspace_bytes(rows: int, cols: int) -> int:
@@ -395,16 +422,22 @@ def nvfp4_rmsnorm_bwd(dy: torch.Tensor, h, gain: Optional[torch.Tensor], rstd: t
                       dgain: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                       residual_grad: Optional[torch.Tensor] = None, accumulate_dgain: bool = False) -> None:
     """h: the kept sum, a bf16 or binary32 tensor or its MXFP8 copy."""
-    rows, cols = dy.shape
-    copy = isinstance(h, NVFP4Tensor)
-    assert residual_grad is None or residual_grad.dtype == dh.dtype
-    _check(lib().nvfp4_rmsnorm_bwd(
-        dy.data_ptr(), _matrix(dy, rows, cols, torch.bfloat16), None if copy else h.data_ptr(),
-        0 if copy else _matrix(h, rows, cols, *_BF16_OR_FP32), not copy and h.dtype == torch.float32, h.packed() if copy else None,
-        _vector(gain, cols), _vector(rstd, rows), rows, cols, _ptr(residual_grad),
-        _matrix(residual_grad, rows, cols, *_BF16_OR_FP32) if residual_grad is not None else 0,
-        dh.data_ptr(), _matrix(dh, rows, cols, *_BF16_OR_FP32), dh.dtype == torch.float32, _vector(dgain, cols), accumulate_dgain,
-        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nvfp4_rmsnorm_bwd")
+    dev, shape = _device(), dy.shape
+    rows, cols = shape
+    lddy = _matrix(dy, shape, dev)
+    ph = ldh = h32 = prg = ldrg = 0
+    h8 = None
+    if isinstance(h, NVFP4Tensor):
+        h8 = _copy8(h, dev)
+    else:
+        ph, ldh, h32 = h.data_ptr(), _matrix(h, shape, dev, _BF16_OR_FP32), h.dtype == torch.float32
+    if residual_grad is not None:
+        assert residual_grad.dtype == dh.dtype
+        prg, ldrg = residual_grad.data_ptr(), _matrix(residual_grad, shape, dev, _BF16_OR_FP32)
+    ws, nws = _scratch(workspace, dev)
+    _check(lib().nvfp4_rmsnorm_bwd(dy.data_ptr(), lddy, ph, ldh, h32, h8, _vector(gain, cols, dev), _vector(rstd, rows, dev), rows, cols,
+                                   prg, ldrg, dh.data_ptr(), _matrix(dh, shape, dev, _BF16_OR_FP32), dh.dtype == torch.float32,
+                                   _vector(dgain, cols, dev), accumulate_dgain, ws, nws, _stream()), "nvfp4_rmsnorm_bwd")
 
 
 _EPILOGUE_FIELDS = struct.Struct("PPqPqPii")  # nvfp4_epilogue
@@ -413,18 +446,20 @@ _EPILOGUE_FIELDS = struct.Struct("PPqPqPii")  # nvfp4_epilogue
 def nvfp4_gemm_bf16_epilogue(A: torch.Tensor, B: torch.Tensor, D: torch.Tensor, bias: Optional[torch.Tensor] = None,
                              act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, z=None) -> None:
     """z = A B^T + bias, D = act(z) + residual (A [M x K], B [N x K]); z: a bf16 tensor or an MXFP8 copy that is to keep it."""
-    M, N = D.shape
+    dev, shape = _device(), D.shape
+    M, N = shape
     K = A.shape[1]
-    copy = z.packed() if isinstance(z, NVFP4Tensor) else None
-    plain_z = z if copy is None else None
-    held = ctypes.c_char_p(copy)  # (the struct's address; held until the call returns)
-    epilogue = _EPILOGUE_FIELDS.pack(
-        _vector(bias, N) or 0, _ptr(residual) or 0, _matrix(residual, M, N, torch.bfloat16) if residual is not None else 0,
-        _ptr(plain_z) or 0, _matrix(plain_z, M, N, torch.bfloat16) if plain_z is not None else 0,
-        (ctypes.cast(held, ctypes.c_void_p).value or 0) if copy is not None else 0, act, 0)
-    _check(lib().nvfp4_gemm_bf16_epilogue(A.data_ptr(), _matrix(A, M, K, torch.bfloat16), B.data_ptr(),
-                                          _matrix(B, N, K, torch.bfloat16), M, N, K, epilogue, D.data_ptr(),
-                                          _matrix(D, M, N, torch.bfloat16), _stream()), "nvfp4_gemm_bf16_epilogue")
+    pr = ldr = pz = ldz = pz8 = 0
+    if residual is not None:
+        pr, ldr = residual.data_ptr(), _matrix(residual, shape, dev)
+    if isinstance(z, NVFP4Tensor):
+        held = ctypes.create_string_buffer(_copy8(z, dev))  # (held until the call returns)
+        pz8 = ctypes.addressof(held)
+    elif z is not None:
+        pz, ldz = z.data_ptr(), _matrix(z, shape, dev)
+    epilogue = _EPILOGUE_FIELDS.pack(_vector(bias, N, dev) or 0, pr, ldr, pz, ldz, pz8, act, 0)
+    _check(lib().nvfp4_gemm_bf16_epilogue(A.data_ptr(), _matrix(A, (M, K), dev), B.data_ptr(), _matrix(B, (N, K), dev), M, N, K,
+                                          epilogue, D.data_ptr(), _matrix(D, shape, dev), _stream()), "nvfp4_gemm_bf16_epilogue")
 
 
 def nvfp4_act_bwd_workspace_bytes(rows: int, cols: int) -> int:
@@ -435,14 +470,22 @@ def nvfp4_act_bwd(da: torch.Tensor, z, act: int, dz: Optional[torch.Tensor] = No
                   dbias: Optional[torch.Tensor] = None, accumulate_dbias: bool = False,
                   workspace: Optional[torch.Tensor] = None) -> None:
     """dz = da act'(z), a = act(z), dbias = column sums of dz; z: a bf16 tensor, its MXFP8 copy, or None where nothing needs it."""
-    rows, cols = da.shape
-    copy = isinstance(z, NVFP4Tensor)
-    plain_z = None if copy else z
-    ld = lambda t: _matrix(t, rows, cols, torch.bfloat16) if t is not None else 0
-    _check(lib().nvfp4_act_bwd(
-        da.data_ptr(), ld(da), _ptr(plain_z), ld(plain_z), z.packed() if copy else None, act, rows, cols, _ptr(dz), ld(dz), _ptr(a),
-        ld(a), _vector(dbias, cols), accumulate_dbias, _ptr(workspace),
-        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nvfp4_act_bwd")
+    dev, shape = _device(), da.shape
+    rows, cols = shape
+    ldda = _matrix(da, shape, dev)
+    pz = ldz = pdz = lddz = pa = lda = 0
+    z8 = None
+    if isinstance(z, NVFP4Tensor):
+        z8 = _copy8(z, dev)
+    elif z is not None:
+        pz, ldz = z.data_ptr(), _matrix(z, shape, dev)
+    if dz is not None:
+        pdz, lddz = dz.data_ptr(), _matrix(dz, shape, dev)
+    if a is not None:
+        pa, lda = a.data_ptr(), _matrix(a, shape, dev)
+    ws, nws = _scratch(workspace, dev)
+    _check(lib().nvfp4_act_bwd(da.data_ptr(), ldda, pz, ldz, z8, act, rows, cols, pdz, lddz, pa, lda, _vector(dbias, cols, dev),
+                               accumulate_dbias, ws, nws, _stream()), "nvfp4_act_bwd")
 
 
 def nvfp4_linear_bf16_bwd8_workspace_bytes(M: int, K: int) -> int:
@@ -452,15 +495,20 @@ def nvfp4_linear_bf16_bwd8_workspace_bytes(M: int, K: int) -> int:
 def nvfp4_linear_bf16_bwd8(dY: torch.Tensor, X8: Optional[NVFP4Tensor], W: Optional[torch.Tensor], dX: Optional[torch.Tensor],
                            dW: Optional[torch.Tensor], workspace: Optional[torch.Tensor] = None, accumulate_dw: bool = False) -> None:
     """Both gradients of a BF16 layer whose input was kept as an MXFP8 copy."""
+    dev = _device()
     M, N = dY.shape
     K = X8.cols if X8 is not None else W.shape[1]
-    assert dY.is_cuda and dY.is_contiguous() and dY.dtype == torch.bfloat16
-    assert dX is None or (W is not None and W.is_contiguous() and W.dtype == torch.bfloat16 and tuple(W.shape) == (N, K)
-                          and dX.is_contiguous() and dX.dtype == torch.bfloat16 and tuple(dX.shape) == (M, K))
-    assert dW is None or (X8 is not None and dW.is_contiguous() and dW.dtype == torch.float32 and tuple(dW.shape) == (N, K))
-    _check(lib().nvfp4_linear_bf16_bwd8(dY.data_ptr(), _ref(X8), _ptr(W), M, N, K, _ptr(dX), _ptr(dW), int(accumulate_dw),
-                                        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                        _stream()), "nvfp4_linear_bf16_bwd8")
+    assert dY.is_contiguous() and _matrix(dY, (M, N), dev) == N
+    pw = pdx = pdw = 0
+    if dX is not None:
+        assert W is not None and W.is_contiguous() and dX.is_contiguous() and _matrix(W, (N, K), dev) == K and _matrix(dX, (M, K), dev) == K
+        pw, pdx = W.data_ptr(), dX.data_ptr()
+    if dW is not None:
+        assert X8 is not None and dW.is_contiguous() and _matrix(dW, (N, K), dev, (torch.float32,)) == K
+        pdw = dW.data_ptr()
+    ws, nws = _scratch(workspace, dev)
+    _check(lib().nvfp4_linear_bf16_bwd8(dY.data_ptr(), _copy8(X8, dev) if X8 is not None else None, pw, M, N, K, pdx, pdw,
+                                        int(accumulate_dw), ws, nws, _stream()), "nvfp4_linear_bf16_bwd8")
 
 
 def nvfp4_rht16(x: torch.Tensor, colwise: bool, sign_mask: int) -> torch.Tensor:

@@ -148,10 +148,10 @@ def test_layer_gradients_from_a_copy():
 
 
 def test_python_calls_refuse_what_is_no_matrix_of_theirs():
-    x = torch.zeros(4, 16, dtype=torch.bfloat16)  # not on a GPU
-    with pytest.raises(AssertionError):
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)  # not on a GPU (and where there is none, the current device cannot be asked for)
+    with pytest.raises((AssertionError, RuntimeError)):
         B.nvfp4_rmsnorm_fwd(x, None, 1e-5, x)
-    with pytest.raises(AssertionError):
+    with pytest.raises((AssertionError, RuntimeError)):
         B.nvfp4_act_bwd(x, x, B.ACT_SILU, x)
-    with pytest.raises(AssertionError):
+    with pytest.raises((AssertionError, RuntimeError)):
         B.nvfp4_gemm_bf16_epilogue(x, x, torch.zeros(4, 4, dtype=torch.bfloat16))
