@@ -747,7 +747,7 @@ template <int BN, int SPLIT, bool TWO, class E = dense::NoEpilogue>
 static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemmArgs* g1, const Bf16Wide& wide_cols, int max_pairs,
                                         cudaStream_t s, const E& epilogue = E{}) {
   auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO, E>;
-  constexpr int smem = dense::Cfg<BN, SPLIT>::kSmemBytes + E::kSmemBytes;
+  constexpr int smem = dense::Cfg<BN, SPLIT>::kSmemBytes + E::kSmemBytes - (E::kBuffers ? dense::Cfg<BN, SPLIT>::kStageBytes : 0);
   static_assert(smem <= 232448, "shared memory budget");
   CUtensorMap m[6];
   if (!make_bf16_maps<BN, SPLIT>(g0, m)) return cudaErrorInvalidValue;
@@ -790,10 +790,10 @@ static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemm
   return e;
 }
 
-template <int BN, int SPLIT = 1>
+template <int BN, int SPLIT = 1, class E = dense::Epilogue>
 static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& a, const Bf16Wide& wide_cols, int max_pairs,
                                         cudaStream_t s) {
-  dense::Epilogue e{};
+  E e{};
   auto map_of = [&](CUtensorMap* map, const void* p, int64_t ld) {
     return make_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, (uint64_t)g.N, (uint64_t)g.M, (uint64_t)ld * 2, SPLIT == 4 ? 32 : 64,
                        128, SPLIT == 4 ? 2 : 1);
@@ -806,7 +806,7 @@ static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueAr
   e.act = a.act;
   e.has_residual = a.residual != nullptr;
   e.has_z = a.z != nullptr;
-  return launch_bf16_problems<BN, SPLIT, false, dense::Epilogue>(g, nullptr, wide_cols, max_pairs, s, e);
+  return launch_bf16_problems<BN, SPLIT, false, E>(g, nullptr, wide_cols, max_pairs, s, e);
 }
 
 // g1 == nullptr: one problem
@@ -876,7 +876,11 @@ cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs
   if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4>(g, e, wide, pairs, s);
   if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2>(g, e, wide, pairs, s);
   if (tile == kTilePair128) return launch_bf16_epilogue<128>(g, e, wide, pairs, s);
-  return tile == kTileDouble ? launch_bf16_epilogue<512>(g, e, wide, pairs, s) : launch_bf16_epilogue<256>(g, e, wide, pairs, s);
+  if (tile == kTileDouble) return launch_bf16_epilogue<512>(g, e, wide, pairs, s);
+  // Buffers for the residual where the main loop is too short to hide its second chunk, K <= 1024; behind longer ones the sixth stage is worth
+  // more.  With the stage / with buffers: 4096 x 5120 x 512 30.9 / 25.5 us (GELU besides 41.3 / 36.3), x 1024 37.1 / 37.6 (46.1 / 42.1), x 1536
+  // 50.5 / 52.4 (54.9 / 56.7), x 4096 132.3 / 133.6 (135.8 / 141.0).
+  return e.residual && g.K <= 1024 ? launch_bf16_epilogue<256, 1, dense::EpilogueBuffers>(g, e, wide, pairs, s) : launch_bf16_epilogue<256>(g, e, wide, pairs, s);
 }
 
 // Test aid: one warp waits, with the given limit, on a barrier nobody arrives at.  The wait runs out, the code lands

@@ -57,11 +57,11 @@ struct Args {
 
 // What follows a product: z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits (a launch with one problem)
 struct NoEpilogue {
-  static constexpr bool kFused = false;
+  static constexpr bool kFused = false, kBuffers = false;
   static constexpr int kSmemBytes = 0;
 };
 struct Epilogue {
-  static constexpr bool kFused = true;
+  static constexpr bool kFused = true, kBuffers = false;
   static constexpr int kSmemBytes = 2 * 128 * 4;  // the bias of a tile's columns, one half per epilogue group
   CUtensorMap map_r, map_z;  // residual and z: the boxes that D is stored in
   const float* bias;
@@ -71,20 +71,36 @@ struct Epilogue {
   int act, has_residual, has_z;
 };
 
+// 256 x 256 tiles with a residual: a stage of the main loop's ring makes room for buffers of 16 KB per epilogue group, so that both chunks
+// of a tile's residual are fetched while its main loop runs.
+struct EpilogueBuffers : Epilogue {
+  static constexpr bool kBuffers = true;
+  static constexpr int kSmemBytes = Epilogue::kSmemBytes + 2 * 16384;
+};
+
 template <int ACT, int COLS>
 __device__ __forceinline__ void activate(uint32_t (&r)[COLS]) {
 #pragma unroll
   for (int j = 0; j < COLS; ++j) r[j] = __float_as_uint(act_value<ACT>(__uint_as_float(r[j])));
 }
 
-// COLS columns of one row as a copy in 8 bits, straight from the registers: a thread has whole blocks, so their maxima need no
-// exchange, and the 32 bytes of a block are a sector.  Columns behind N are zeros in r.
+// COLS columns of one row as a copy in 8 bits, from the registers: a thread has whole blocks, so their maxima need no exchange.  Columns
+// behind N are zeros in r.  Where N is a multiple of 32 a thread stores the 32 bytes of a block, a sector, itself; else the warp turns its 32
+// rows round in the staging buffer and stores them row by row.  The whole group calls; buf: the group's staging buffer.
 template <int COLS>
-__device__ __forceinline__ void store_row8(const uint32_t (&r)[COLS], const Epilogue& e, int64_t row, int x0, int N) {
+__device__ __forceinline__ void store_rows8(const uint32_t (&r)[COLS], const Epilogue& e, int row_in_tile, int row0, int M, int x0, int N,
+                                            bool wide, uint32_t buf, int et, int bar_id) {
+  const int64_t row = row0 + row_in_tile;
+  const bool live = row < M;
   uint32_t bytes = 0;
-  const bool wide = (N & 31) == 0 && (reinterpret_cast<uintptr_t>(e.z8_codes) & 31) == 0;
   uint8_t* const scales = e.z8_scales + row * e.z8_blocks + (x0 >> 5);
   const bool word = COLS == 128 && (e.z8_blocks & 3) == 0;
+  constexpr int kUnits = COLS / 16;  // of 16 codes in a staged row
+  const uint32_t srow = buf + row_in_tile * COLS;
+  if (!wide) {
+    if (et == 0) pair::bulk_wait_read<0>();  // the stores before have read the buffer
+    asm volatile("bar.sync %0, 128;" ::"r"(bar_id) : "memory");
+  }
 #pragma unroll
   for (int b = 0; b < COLS / 32; ++b) {
     const int x = x0 + 32 * b;
@@ -93,50 +109,71 @@ __device__ __forceinline__ void store_row8(const uint32_t (&r)[COLS], const Epil
 #pragma unroll
     for (int j = 0; j < 32; j += 2) m = amax3(m, __uint_as_float(r[32 * b + j]), __uint_as_float(r[32 * b + j + 1]));
     const uint32_t byte = scale_byte8(m);
-    const float scale = encode_scale8(byte);
+    const float2 scale = both(encode_scale8(byte));
     uint32_t w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t* const q = &r[32 * b + 4 * j];
-      w[j] = e4m3x4(__uint_as_float(q[0]) * scale, __uint_as_float(q[1]) * scale, __uint_as_float(q[2]) * scale, __uint_as_float(q[3]) * scale);
+      const float2 lo = mul2(make_float2(__uint_as_float(q[0]), __uint_as_float(q[1])), scale);
+      const float2 hi = mul2(make_float2(__uint_as_float(q[2]), __uint_as_float(q[3])), scale);
+      w[j] = e4m3x4(lo.x, lo.y, hi.x, hi.y);
     }
-    uint8_t* const dst = e.z8_codes + row * N + x;
     if (wide) {
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                   : "memory");
+      if (live)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(e.z8_codes + row * N + x), "r"(w[0]), "r"(w[1]),
+                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (x + 8 * j < N) *reinterpret_cast<uint2*>(dst + 8 * j) = make_uint2(w[2 * j], w[2 * j + 1]);
+      for (int u = 0; u < 2; ++u)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(srow + (((2 * b + u) ^ (row_in_tile & (kUnits - 1))) << 4)),
+                     "r"(w[4 * u]), "r"(w[4 * u + 1]), "r"(w[4 * u + 2]), "r"(w[4 * u + 3])
+                     : "memory");
     }
     if (word)
       bytes |= byte << (8 * b);
-    else
+    else if (live)
       scales[b] = (uint8_t)byte;
   }
-  if (word && x0 < N) *reinterpret_cast<uint32_t*>(scales) = bytes;
+  if (word && live && x0 < N) *reinterpret_cast<uint32_t*>(scales) = bytes;
+  if (wide) return;
+  __syncwarp();
+  constexpr int kPieces = COLS / 8, kRowsAtOnce = 32 / kPieces;  // of eight codes
+  const int lane = row_in_tile & 31, first = row_in_tile - lane, p = lane % kPieces;
+#pragma unroll
+  for (int k = 0; k < 32; k += kRowsAtOnce) {
+    const int rr = first + k + lane / kPieces;
+    if (row0 + rr < M && x0 + 8 * p < N)
+      *reinterpret_cast<uint2*>(e.z8_codes + (int64_t)(row0 + rr) * N + x0 + 8 * p) =
+          lds8(buf + rr * COLS + (((p >> 1) ^ (rr & (kUnits - 1))) << 4) + 8 * (p & 1));
+  }
+  // what comes into the buffer next, by a thread or by TMA, comes behind these reads
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  asm volatile("bar.sync %0, 128;" ::"r"(bar_id) : "memory");
 }
 
 // Units of 16 bytes of a staged row, as store_half() has them for bf16
 template <int COLS>
 constexpr int kStagedUnits = COLS < 64 ? 4 : 8;
 
-// The residual of the next chunk into the group's staging buffer, once the store before has read it (one thread)
+// A chunk of the residual into a buffer of the group, once the stores before have read it (one thread)
 template <int COLS>
-__device__ __forceinline__ void load_residual(const Epilogue& e, uint32_t stage_buf, int x, int row0, uint32_t res_bar) {
+__device__ __forceinline__ void load_residual(const Epilogue& e, uint32_t buf, int x, int row0, uint32_t res_bar) {
   pair::bulk_wait_read<0>();
   mbar_expect_tx(res_bar, 128 * 16 * kStagedUnits<COLS>);
-  tma_load_2d(stage_buf, &e.map_r, x, row0, res_bar);
+  tma_load_2d(buf, &e.map_r, x, row0, res_bar);
 }
+// z, or a copy of it that a warp turns round, goes through the staging buffer before the residual may come there
+__device__ __forceinline__ bool z_is_staged(const Epilogue& e, bool wide8) { return e.has_z || (e.z8_codes && !wide8); }
 
-// The epilogue of COLS columns of one row per thread.  The residual comes by TMA into the staging buffer, in the place from which the
-// sum then leaves: a thread reads and writes its own row.  prefetched: the first chunk is on its way.  false: a wait ran out (all 128
-// threads agree).
-template <int COLS>
+// The epilogue of COLS columns of one row per thread.  The residual comes by TMA, chunk c into the staging buffer (BUFFERS: the second into
+// res_buf), in the place from which the sum then leaves: a thread reads and writes its own row.  prefetched: the first chunk (BUFFERS: the
+// second in any case) is on its way.  false: a wait ran out (all 128 threads agree).
+template <int COLS, bool BUFFERS>
 __device__ __forceinline__ bool finish_half(uint32_t (&r)[COLS], const Epilogue& e, const float* bias, int M, int N, int et, int bar_id,
-                                            int row_in_tile, uint32_t stage_buf, const CUtensorMap* map_d, int x0, int row0,
-                                            uint32_t res_bar, uint32_t& res_phase, bool prefetched, volatile uint32_t* abort_flag) {
+                                            int row_in_tile, uint32_t stage_buf, uint32_t res_buf, const CUtensorMap* map_d, int x0,
+                                            int row0, uint32_t res_bar, uint32_t& res_phase, bool wide8, bool prefetched,
+                                            volatile uint32_t* abort_flag) {
   if (e.bias) {
 #pragma unroll
     for (int j = 0; j < COLS; j += 4) {
@@ -147,7 +184,7 @@ __device__ __forceinline__ bool finish_half(uint32_t (&r)[COLS], const Epilogue&
       r[j + 3] = __float_as_uint(__uint_as_float(r[j + 3]) + b.w);
     }
   }
-  if (e.z8_codes && row0 + row_in_tile < M) store_row8<COLS>(r, e, row0 + row_in_tile, x0, N);
+  if (e.z8_codes) store_rows8<COLS>(r, e, row_in_tile, row0, M, x0, N, wide8, stage_buf, et, bar_id);
   if (e.has_z) pair::store_half<false, false, COLS>(r, 1.0f, et, bar_id, row_in_tile, stage_buf, &e.map_z, x0, row0, 0, false);
   switch (e.act) {
     case NVFP4_ACT_RELU2: activate<NVFP4_ACT_RELU2>(r); break;
@@ -162,11 +199,13 @@ __device__ __forceinline__ bool finish_half(uint32_t (&r)[COLS], const Epilogue&
   constexpr int kUnits = kStagedUnits<COLS>, kChunkCols = 8 * kUnits;
 #pragma unroll
   for (int c = 0; c < COLS / kChunkCols; ++c) {
-    if (et == 0 && !(c == 0 && prefetched)) load_residual<COLS>(e, stage_buf, x0 + c * kChunkCols, row0, res_bar);
-    mbar_wait(res_bar, res_phase, abort_flag, 0xE00u);
-    res_phase ^= 1u;
+    const bool second = BUFFERS && c == 1;
+    const uint32_t buf = second ? res_buf : stage_buf, bar = res_bar + (second ? 16u : 0u);
+    if (et == 0 && !second && !(c == 0 && prefetched)) load_residual<COLS>(e, buf, x0 + c * kChunkCols, row0, bar);
+    mbar_wait(bar, (res_phase >> (second ? 1 : 0)) & 1u, abort_flag, 0xE00u);
+    res_phase ^= second ? 2u : 1u;
     if (group_gave_up(abort_flag, bar_id, 128)) return false;
-    const uint32_t srow = stage_buf + row_in_tile * (16 * kUnits);
+    const uint32_t srow = buf + row_in_tile * (16 * kUnits);
     const uint32_t x = kUnits == 4 ? (row_in_tile >> 1) & 3 : row_in_tile & 7;  // (the swizzles of store_half)
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
@@ -183,7 +222,7 @@ __device__ __forceinline__ bool finish_half(uint32_t (&r)[COLS], const Epilogue&
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     asm volatile("bar.sync %0, 128;" ::"r"(bar_id) : "memory");
     if (et == 0) {
-      pair::tma_store_2d(map_d, x0 + c * kChunkCols, row0, stage_buf);
+      pair::tma_store_2d(map_d, x0 + c * kChunkCols, row0, buf);
       pair::bulk_commit();
     }
   }
@@ -215,7 +254,7 @@ __device__ __forceinline__ void tc2_mma_bf16(uint32_t d_tmem, uint64_t adesc, ui
 // SPLIT > 1 (BN = 128): a cluster of SPLIT pairs takes one tile, the only one of its life,
 // each pair a share of the k-blocks (the exchange: pair::exchange_columns).
 // TWO: the launch has two problems.
-// E: Epilogue or NoEpilogue.
+// E: Epilogue (EpilogueBuffers) or NoEpilogue.
 template <int BN, int SPLIT = 1, bool TWO = true, class E = NoEpilogue>
 __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_bf16_pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
@@ -224,23 +263,25 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
                           const __grid_constant__ Args g, const __grid_constant__ E e) {
   static_assert(!E::kFused || !TWO, "an epilogue belongs to one product");
   using namespace pair;
-  constexpr int S = dense::Cfg<BN, SPLIT>::kStages, kStageBytes = dense::Cfg<BN, SPLIT>::kStageBytes;
+  static_assert(!E::kBuffers || (BN == 256 && SPLIT == 1), "two chunks to a group");
+  constexpr int S = dense::Cfg<BN, SPLIT>::kStages - (E::kBuffers ? 1 : 0), kStageBytes = dense::Cfg<BN, SPLIT>::kStageBytes;
   constexpr bool kDouble = BN == 512;        // two 256-column halves
   constexpr int HN = kDouble ? 256 : BN;     // columns of an accumulator
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t staging = base + S * kStageBytes;
-  const uint32_t bar_base = staging + dense::kStagingBytes;
+  constexpr int kBarOffset = S * kStageBytes + dense::kStagingBytes + (E::kBuffers ? 32768 : 0);
+  const uint32_t bar_base = base + kBarOffset;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };              // leader only: both CTAs' operands landed
   auto empty_bar = [&](int s) { return bar_base + 8u * (S + s); };       // one per CTA
   auto accf_bar = [&](int b) { return bar_base + 8u * (2 * S + b); };    // one per CTA and accumulator
   auto acce_bar = [&](int b) { return bar_base + 8u * (2 * S + 2 + b); };  // leader only, 16 arrivals
   const uint32_t done_bar = bar_base + 8u * (2 * S + 4);
   const uint32_t recv_bar = done_bar + 16;                               // SPLIT > 1: all shares are here
-  auto res_bar = [&](int group) { return done_bar + 24u + 8u * group; };  // E: a chunk of the residual is here
+  auto res_bar = [&](int group) { return done_bar + 24u + 8u * group; };  // E: a chunk of the residual is here (kBuffers: the second, + 16)
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(
-      base_ptr + S * kStageBytes + dense::kStagingBytes + 8 * (2 * S + 5));
+      base_ptr + kBarOffset + 8 * (2 * S + 5));
   volatile uint32_t* abort_flag = tmem_slot + 1;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -304,7 +345,7 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     mbar_init(done_bar, 2 * SPLIT - 1);
     if (SPLIT > 1) mbar_init(recv_bar, 1);
     if (E::kFused)
-      for (int b = 0; b < 2; ++b) mbar_init(res_bar(b), 1);
+      for (int b = 0; b < 4; ++b) mbar_init(res_bar(b), 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -480,9 +521,15 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     const int row_in_tile = quad * 32 + lane;
     const uint32_t stage_buf = staging + half * 16384;
     int buf = 0, last_prob = 0, halves = 1;
-    [[maybe_unused]] uint32_t res_phase = 0;
+    [[maybe_unused]] uint32_t res_phase = 0;  // bit c: phase of chunk c's barrier
+    [[maybe_unused]] bool wide8 = false, early = false;
+    if constexpr (E::kFused) {
+      wide8 = (g.p[0].N & 31) == 0 && (reinterpret_cast<uintptr_t>(e.z8_codes) & 31) == 0;
+      early = SPLIT == 1 && !z_is_staged(e, wide8);
+    }
     [[maybe_unused]] float* const bias_s = reinterpret_cast<float*>(
-        base_ptr + S * kStageBytes + dense::kStagingBytes + 256 + dense::Cfg<BN, SPLIT>::kRecvBytes) + half * 128;
+        base_ptr + kBarOffset + 256 + dense::Cfg<BN, SPLIT>::kRecvBytes) + half * 128;
+    [[maybe_unused]] const uint32_t res_buf = staging + dense::kStagingBytes + half * 16384;  // (kBuffers)
     // (kDouble: a tile comes up once for each of its halves, the second time without a step of the walk)
     for (int rnd = 0, half_no = 0, tile = pair_id; tile < n_tiles; tile = half_no ? tile : next_tile(++rnd)) {
       int prob, m_blk, n_blk;
@@ -502,8 +549,11 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
         const int x0 = SPLIT > 1 ? n_blk * BN + split * kCols : n_blk * HN + half * kCols;
         // (the threads are behind the barriers of the tile before, and so behind their reads of its bias)
         if (e.bias && et < kCols) bias_s[et] = x0 + et < g.p[0].N ? e.bias[x0 + et] : 0.f;
-        if (SPLIT == 1 && e.has_residual && !e.has_z && et == 0)
-          load_residual<kCols>(e, stage_buf, x0, m_blk * 256 + (int)rank * 128, res_bar(half));
+        if (et == 0 && e.has_residual) {
+          const int row0 = m_blk * 256 + (int)rank * 128;
+          if (early) load_residual<kCols>(e, stage_buf, x0, row0, res_bar(half));
+          if (E::kBuffers) load_residual<kCols>(e, res_buf, x0 + kCols / 2, row0, res_bar(half) + 16);
+        }
       }
       mbar_wait_cluster(accf_bar(buf), (acc_phase >> buf) & 1u, abort_flag, 0xC00u + buf);
       // agree on giving up: a warp that timed out still joins this barrier, and all 128 threads take ONE decision
@@ -526,16 +576,16 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
           break;
         const int xs = n_blk * BN + split * kCols;
         if constexpr (E::kFused) {
-          if (!finish_half<kCols>(v, e, bias_s, g.p[0].M, g.p[0].N, et, bar_id, row_in_tile, stage_buf, map_d, xs, row0, res_bar(half),
-                                  res_phase, false, abort_flag))
+          if (!finish_half<kCols, false>(v, e, bias_s, g.p[0].M, g.p[0].N, et, bar_id, row_in_tile, stage_buf, 0, map_d, xs, row0,
+                                         res_bar(half), res_phase, wide8, false, abort_flag))
             break;
         } else if (g.p[prob].d_is_fp32)
           store_half<true, false, kCols>(v, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, xs, row0, g.p[prob].accumulate, drain);
         else
           store_half<false, false, kCols>(v, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, xs, row0, g.p[prob].accumulate, drain);
       } else if constexpr (E::kFused) {
-        if (!finish_half<HN / 2>(r, e, bias_s, g.p[0].M, g.p[0].N, et, bar_id, row_in_tile, stage_buf, map_d, n_blk * HN + half * (HN / 2),
-                                 row0, res_bar(half), res_phase, !e.has_z, abort_flag))
+        if (!finish_half<HN / 2, E::kBuffers>(r, e, bias_s, g.p[0].M, g.p[0].N, et, bar_id, row_in_tile, stage_buf, res_buf, map_d,
+                                              n_blk * HN + half * (HN / 2), row0, res_bar(half), res_phase, wide8, early, abort_flag))
           break;
       } else if (g.p[prob].d_is_fp32)
         store_half<true, false, HN / 2>(r, 1.0f, et, bar_id, row_in_tile, stage_buf, map_d, n_blk * HN + half * (HN / 2),
