@@ -345,7 +345,8 @@ typedef struct nvfp4_epilogue {
 } nvfp4_epilogue;
 /*
  * nvfp4_gemm_bf16_epilogue: the product of nvfp4_gemm_bf16 for K-major operands (X [M x K], W [N x K]) with the above in its epilogue,
- *   in binary32 until D (bf16) is rounded.  M any number from one on; N, K multiples of 8; lda, ldb, ldd, ldr, ldz multiples of 8; pointers
+ *   in binary32 until D (bf16) is rounded (with z8, sums of 1024 products are added up rounded to nearest, as in nvfp4_linear_bf16_bwd8).
+ *   M any number from one on; N, K multiples of 8; lda, ldb, ldd, ldr, ldz multiples of 8; pointers
  *   16-byte aligned.
  * nvfp4_act_bwd: dz = da * act'(z) (bf16), a = act(z) (bf16: the next layer's input made again for its weight gradient),
  *   dbias = (accumulate_dbias ? dbias : 0) + sum over the rows of dz before its rounding.
@@ -353,7 +354,8 @@ typedef struct nvfp4_epilogue {
  *   be NULL, not all; dz may be da itself and a may be z itself (same leading dimensions).
  *   workspace: nvfp4_act_bwd_workspace_bytes(rows, cols), 256-byte aligned, for dbias (NULL without).
  * nvfp4_linear_bf16_bwd8: nvfp4_linear_bf16_bwd with X from its MXFP8 copy [M x K]: dW = dY^T X^, X^ the copy's values in bf16 (exact
- *   but below 2^-126).  Same bits as nvfp4_dequantize_bf16 followed by nvfp4_linear_bf16_bwd.
+ *   but below 2^-126).  dW adds up sums of 1024 products, rounded to nearest, where nvfp4_linear_bf16_bwd leaves the whole sum to the tensor
+ *   cores, which cut it off at every addition.
  *   workspace: nvfp4_linear_bf16_bwd8_workspace_bytes(M, K), 256-byte aligned, for X^ (NULL without dW).
  * nvfp4_dequantize_bf16: the values of an MXFP8 copy in bf16, leading dimension ld.
  */

@@ -561,27 +561,39 @@ nvfp4_status nvfp4_gemm_bf16_epilogue(const void* A, int64_t lda, const void* B,
   return launch_gemm_bf16_epilogue(g, e, tile, wide, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
 }
 
-size_t nvfp4_linear_bf16_bwd8_workspace_bytes(int64_t M, int64_t K) { return M > 0 && K > 0 ? align_up((size_t)M * (size_t)K * 2, 256) : 0; }
+// X^ has rows of whole 64 bytes: as an operand, rows that begin on 32 bytes are loaded faster (see bf16_schedule.h)
+static int64_t bwd8_ld(int64_t K) { return (K + 31) / 32 * 32; }
+size_t nvfp4_linear_bf16_bwd8_workspace_bytes(int64_t M, int64_t K) {
+  return M > 0 && K > 0 ? align_up((size_t)M * (size_t)bwd8_ld(K) * 2, 256) : 0;
+}
 
 nvfp4_status nvfp4_linear_bf16_bwd8(const void* dY, const nvfp4_tensor* X8, const void* W, int64_t M, int64_t N, int64_t K,
                                     void* dX_bf16, float* dW_fp32, int32_t accumulate_dw, void* workspace, size_t workspace_bytes,
                                     void* cuda_stream) {
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (!dY) return NVFP4_ERR_NULL;
   if (!dX_bf16 && !dW_fp32) return NVFP4_ERR_NULL;
   if (dW_fp32 && !X8) return NVFP4_ERR_NULL;
   if (M <= 0 || N <= 0 || K <= 0 || M > 0x7fffff00 || N > 0x7fffff00 || K > 0x7fffff00) return NVFP4_ERR_SHAPE;
   nvfp4_status st;
-  DenseGemmArgs g;  // every step is validated before the first launch
-  if (dX_bf16 && (st = bf16_prepare(dY, NVFP4_K_MAJOR, N, W, NVFP4_MN_MAJOR, K, M, K, N, dX_bf16, 0, K, 0, g)) != NVFP4_OK) return st;
-  if (dW_fp32) {
-    if ((st = check_copy8(X8, M, K)) != NVFP4_OK) return st;
-    if (!workspace || workspace_bytes < nvfp4_linear_bf16_bwd8_workspace_bytes(M, K)) return NVFP4_ERR_WORKSPACE;
-    if (!aligned(workspace, 256)) return NVFP4_ERR_ALIGN;
-    if ((st = bf16_prepare(dY, NVFP4_MN_MAJOR, N, workspace, NVFP4_MN_MAJOR, K, N, K, M, dW_fp32, 1, K, accumulate_dw, g)) != NVFP4_OK)
-      return st;
-    if (launch_dequantize8(*X8, workspace, false, K, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return NVFP4_ERR_CUDA;
-  }
-  return nvfp4_linear_bf16_bwd(dY, workspace, W, M, N, K, dX_bf16, dW_fp32, accumulate_dw, cuda_stream);
+  DenseGemmArgs gd, gw;  // every step is validated before the first launch
+  if (dX_bf16 && (st = bf16_prepare(dY, NVFP4_K_MAJOR, N, W, NVFP4_MN_MAJOR, K, M, K, N, dX_bf16, 0, K, 0, gd)) != NVFP4_OK) return st;
+  if (!dW_fp32) return bf16_impl(gd, nullptr, cuda_stream);
+  if ((st = check_copy8(X8, M, K)) != NVFP4_OK) return st;
+  if (!workspace || workspace_bytes < nvfp4_linear_bf16_bwd8_workspace_bytes(M, K)) return NVFP4_ERR_WORKSPACE;
+  if (!aligned(workspace, 256)) return NVFP4_ERR_ALIGN;
+  if ((st = bf16_prepare(dY, NVFP4_MN_MAJOR, N, workspace, NVFP4_MN_MAJOR, bwd8_ld(K), N, K, M, dW_fp32, 1, K, accumulate_dw, gw)) != NVFP4_OK)
+    return st;
+  if (launch_dequantize8(*X8, workspace, false, bwd8_ld(K), s) != cudaSuccess) return NVFP4_ERR_CUDA;
+  // Both products in one launch fill each other's last round, unless dX alone would have 512-wide tiles, which the other's sums outside the
+  // tensor cores leave no accumulator for: 8192 x 2056 x 5128 in one launch 345 us, apart 302, 4088 x 5128 x 5112 359 / 350.
+  const int forced = g_tile_n.load(std::memory_order_relaxed);
+  Bf16Wide wide;
+  const int tile_d = dX_bf16 ? bf16_tile(gd, nullptr, forced, &wide) : 0;
+  if (dX_bf16 && tile_d == kTileDouble && launch_gemm_bf16(gd, nullptr, tile_d, wide, s) != cudaSuccess) return NVFP4_ERR_CUDA;
+  const bool both = dX_bf16 && tile_d != kTileDouble, dgrad_first = both && gd.K >= gw.K;
+  const DenseGemmArgs &g0 = dgrad_first ? gd : gw, *g1 = both ? (dgrad_first ? &gw : &gd) : nullptr;
+  return launch_gemm_bf16_shares(g0, g1, bf16_tile(g0, g1, forced, &wide), s) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
 }
 
 nvfp4_status nvfp4_quant_error(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, const nvfp4_tensor* q,

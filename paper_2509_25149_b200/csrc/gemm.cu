@@ -743,10 +743,10 @@ static bool make_bf16_maps(const DenseGemmArgs& g, CUtensorMap* m) {  // A, B, D
 
 static int bf16_tiles(const DenseGemmArgs& g, int bn) { return ((g.M + 255) / 256) * ((g.N + bn - 1) / bn); }
 
-template <int BN, int SPLIT, bool TWO, class E = dense::NoEpilogue>
+template <int BN, int SPLIT, bool TWO, class E = dense::NoEpilogue, int SHARE = 0>
 static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemmArgs* g1, const Bf16Wide& wide_cols, int max_pairs,
                                         cudaStream_t s, const E& epilogue = E{}) {
-  auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO, E>;
+  auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO, E, SHARE>;
   constexpr int smem = dense::Cfg<BN, SPLIT>::kSmemBytes + E::kSmemBytes - (E::kBuffers ? dense::Cfg<BN, SPLIT>::kStageBytes : 0);
   static_assert(smem <= 232448, "shared memory budget");
   CUtensorMap m[6];
@@ -790,7 +790,7 @@ static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemm
   return e;
 }
 
-template <int BN, int SPLIT = 1, class E = dense::Epilogue>
+template <int BN, int SPLIT = 1, class E = dense::Epilogue, int SHARE = 0>
 static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& a, const Bf16Wide& wide_cols, int max_pairs,
                                         cudaStream_t s) {
   E e{};
@@ -806,15 +806,15 @@ static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueAr
   e.act = a.act;
   e.has_residual = a.residual != nullptr;
   e.has_z = a.z != nullptr;
-  return launch_bf16_problems<BN, SPLIT, false, E>(g, nullptr, wide_cols, max_pairs, s, e);
+  return launch_bf16_problems<BN, SPLIT, false, E, SHARE>(g, nullptr, wide_cols, max_pairs, s, e);
 }
 
 // g1 == nullptr: one problem
-template <int BN, int SPLIT = 1>
+template <int BN, int SPLIT = 1, int SHARE = 0>
 static cudaError_t launch_bf16_t(const DenseGemmArgs& g0, const DenseGemmArgs* g1, const Bf16Wide& wide_cols, int max_pairs,
                                  cudaStream_t s) {
-  return g1 ? launch_bf16_problems<BN, SPLIT, true>(g0, g1, wide_cols, max_pairs, s)
-            : launch_bf16_problems<BN, SPLIT, false>(g0, nullptr, wide_cols, max_pairs, s);
+  return g1 ? launch_bf16_problems<BN, SPLIT, true, dense::NoEpilogue, SHARE>(g0, g1, wide_cols, max_pairs, s)
+            : launch_bf16_problems<BN, SPLIT, false, dense::NoEpilogue, SHARE>(g0, nullptr, wide_cols, max_pairs, s);
 }
 
 static Bf16Wide bf16_wide_tiles(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int pairs) {
@@ -868,11 +868,29 @@ cudaError_t launch_gemm_bf16(const DenseGemmArgs& g0, const DenseGemmArgs* g1, i
   return tile == kTileDouble ? launch_bf16_t<512>(g0, g1, wide, pairs, s) : launch_bf16_t<256>(g0, g1, wide, pairs, s);
 }
 
+cudaError_t launch_gemm_bf16_shares(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, cudaStream_t s) {
+  int num_sms = 0;
+  const cudaError_t e = sm_count(&num_sms);
+  if (e != cudaSuccess) return e;
+  const int pairs = num_sms / 2;
+  const Bf16Wide none{{0, 0}};
+  if (tile == kTileSplit4) return launch_bf16_t<128, 4, dense::kShare>(g0, g1, none, pairs, s);
+  if (tile == kTileSplit2) return launch_bf16_t<128, 2, dense::kShare>(g0, g1, none, pairs, s);
+  if (tile == kTilePair128) return launch_bf16_t<128, 1, dense::kShare>(g0, g1, none, pairs, s);
+  return launch_bf16_t<256, 1, dense::kShare>(g0, g1, none, pairs, s);
+}
+
 cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& e, int tile, const Bf16Wide& wide, cudaStream_t s) {
   int num_sms = 0;
   const cudaError_t err = sm_count(&num_sms);
   if (err != cudaSuccess) return err;
   const int pairs = num_sms / 2;
+  if (e.z8_codes) {
+    if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4, dense::Epilogue, dense::kShare>(g, e, wide, pairs, s);
+    if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2, dense::Epilogue, dense::kShare>(g, e, wide, pairs, s);
+    if (tile == kTilePair128) return launch_bf16_epilogue<128, 1, dense::Epilogue, dense::kShare>(g, e, wide, pairs, s);
+    return launch_bf16_epilogue<256, 1, dense::Epilogue, dense::kShare>(g, e, Bf16Wide{{0, 0}}, pairs, s);
+  }
   if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4>(g, e, wide, pairs, s);
   if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2>(g, e, wide, pairs, s);
   if (tile == kTilePair128) return launch_bf16_epilogue<128>(g, e, wide, pairs, s);

@@ -76,6 +76,8 @@ struct DenseGemmArgs {
 // The tile of such a launch: kTilePair256, kTilePair128, kTileDouble (*wide: how many column tiles of each product are 512 wide) or a
 // split one (`forced`, where every share has a k-block, or by size)
 int bf16_tile(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int forced, Bf16Wide* wide);
+// The same with sums of 1024 products at most added up outside the tensor cores (SHARE in gemm_bf16.cuh); no 512-wide tiles
+cudaError_t launch_gemm_bf16_shares(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, cudaStream_t s);
 // What follows a product (nvfp4_gemm_bf16_epilogue): z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits
 struct EpilogueArgs {
   const float* bias;

@@ -255,13 +255,23 @@ __device__ __forceinline__ void tc2_mma_bf16(uint32_t d_tmem, uint64_t adesc, ui
 // each pair a share of the k-blocks (the exchange: pair::exchange_columns).
 // TWO: the launch has two problems.
 // E: Epilogue (EpilogueBuffers) or NoEpilogue.
-template <int BN, int SPLIT = 1, bool TWO = true, class E = NoEpilogue>
+// SHARE > 0: an accumulator takes no more than SHARE k-blocks.  Then the issuer goes on in the other one, and the epilogue warps add what it
+// holds to sums of their own, rounded to nearest.  The tensor cores cut off what an addition to an accumulator cannot hold, an error that
+// grows with every one of them: a weight gradient over 16384 tokens (values of an 8-bit copy) is 8.6e-6 off in the mean square, 3.1e-5 where all
+// terms have one sign; in shares of 8 / 16 k-blocks 1.9e-7 / 2.3e-7 and 3.9e-7 / 6.3e-7.  What it costs is the power of reading the
+// accumulators more often (8192 x 20480 x 5120 with codes of 8 bits, at the power limit: 1370 us in one sum, 1419 in shares of 16, 1505 of
+// 8) and, where a share is as short as the epilogue of the tile before, waiting for that.  Of such codes 1.7 times as many come out a step off
+// as with sums in binary32 in shares of 16, as many in shares of 8, three times as many in shares of 32.
+// Not for 512-wide tiles, whose halves need both accumulators.
+constexpr int kShare = 16;
+template <int BN, int SPLIT = 1, bool TWO = true, class E = NoEpilogue, int SHARE = 0>
 __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_bf16_pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
                           const __grid_constant__ CUtensorMap map_d0, const __grid_constant__ CUtensorMap map_a1,
                           const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_d1,
                           const __grid_constant__ Args g, const __grid_constant__ E e) {
   static_assert(!E::kFused || !TWO, "an epilogue belongs to one product");
+  static_assert(SHARE == 0 || BN < 512, "two accumulators in turn");
   using namespace pair;
   static_assert(!E::kBuffers || (BN == 256 && SPLIT == 1), "two chunks to a group");
   constexpr int S = dense::Cfg<BN, SPLIT>::kStages - (E::kBuffers ? 1 : 0), kStageBytes = dense::Cfg<BN, SPLIT>::kStageBytes;
@@ -491,8 +501,15 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
             }
           }
           for (int kb = 0; kb < k_blocks; ++kb) {
+            if (SHARE > 0 && kb > 0 && kb % (SHARE > 0 ? SHARE : 1) == 0) {  // this share is complete; on in the other accumulator
+              tc2_commit_both(accf_bar(buf), pair_mask);
+              acc_phase ^= 1u << buf;
+              buf ^= 1;
+              if (!(ok = acc_free(buf))) return;
+              tc_fence_after();
+            }
             if (!landed(stage, phase)) return;
-            mma(stage, 0, buf, kb == 0);
+            mma(stage, 0, buf, SHARE > 0 ? kb % (SHARE > 0 ? SHARE : 1) == 0 : kb == 0);
             release();
           }
         };
@@ -555,19 +572,48 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
           if (E::kBuffers) load_residual<kCols>(e, res_buf, x0 + kCols / 2, row0, res_bar(half) + 16);
         }
       }
-      mbar_wait_cluster(accf_bar(buf), (acc_phase >> buf) & 1u, abort_flag, 0xC00u + buf);
-      // agree on giving up: a warp that timed out still joins this barrier, and all 128 threads take ONE decision
-      if (group_gave_up(abort_flag, bar_id, 128)) break;
-      tc_fence_after();
       const int row0 = m_blk * 256 + (int)rank * 128;
-      const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256 + half * (HN / 2);
       uint32_t r[HN / 2];
+      if constexpr (SHARE > 0) {
+        const int shares = (k_begin(tile, split + 1) - k_begin(tile, split) + SHARE - 1) / SHARE;
+        bool gave_up = false;
 #pragma unroll
-      for (int q = 0; q < HN / 32; ++q) tc_ld16(t_row + q * 16, *reinterpret_cast<uint32_t(*)[16]>(&r[q * 16]));
-      tc_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_cta(acce_bar(buf), leader_cta));
+        for (int j = 0; j < HN / 2; ++j) r[j] = 0u;
+        for (int share = 0; share < shares; ++share) {
+          mbar_wait_cluster(accf_bar(buf), (acc_phase >> buf) & 1u, abort_flag, 0xC00u + buf);
+          if ((gave_up = group_gave_up(abort_flag, bar_id, 128))) break;
+          tc_fence_after();
+          const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256 + half * (HN / 2);
+#pragma unroll
+          for (int q = 0; q < HN / 32; ++q) {
+            uint32_t t[16];  // (with 32 at a time the registers did not suffice)
+            tc_ld16(t_row + q * 16, t);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) r[q * 16 + j] = __float_as_uint(__uint_as_float(r[q * 16 + j]) + __uint_as_float(t[j]));
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(acce_bar(buf), leader_cta));
+          if (share + 1 < shares) {  // (the last share's is turned over behind the tile)
+            acc_phase ^= 1u << buf;
+            buf ^= 1;
+          }
+        }
+        if (gave_up) break;
+      } else {
+        mbar_wait_cluster(accf_bar(buf), (acc_phase >> buf) & 1u, abort_flag, 0xC00u + buf);
+        // agree on giving up: a warp that timed out still joins this barrier, and all 128 threads take ONE decision
+        if (group_gave_up(abort_flag, bar_id, 128)) break;
+        tc_fence_after();
+        const uint32_t t_row = tmem + ((uint32_t)(quad * 32) << 16) + buf * 256 + half * (HN / 2);
+#pragma unroll
+        for (int q = 0; q < HN / 32; ++q) tc_ld16(t_row + q * 16, *reinterpret_cast<uint32_t(*)[16]>(&r[q * 16]));
+        tc_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(acce_bar(buf), leader_cta));
+      }
       if constexpr (SPLIT > 1) {
         constexpr int kCols = BN / SPLIT;
         uint32_t v[kCols];
