@@ -302,7 +302,8 @@ NVFP4_API nvfp4_status nvfp4_linear_fwd_noalloc(const void* X, const void* W, in
 /*
  * Around the linear layers: what makes their input, follows their product and is kept for their backward pass.
  * Matrices are row-major with a leading dimension in elements (>= cols); bf16 leading dimensions are multiples of 8, binary32 ones of
- * 4, pointers 16-byte aligned, cols a multiple of 8.  Any number of rows from one on.  Buffers overlap only where it is said that they may.
+ * 4, pointers 16-byte aligned, cols a multiple of 8.  Any number of rows from one on.  Buffers overlap only where it is said that they may,
+ * and calls that may run at the same time (two streams, two captured graphs) need workspaces of their own.
  *
  * nvfp4_rmsnorm_fwd: h = x + residual (one binary32 addition; h = x without a residual), rstd = 1 / sqrt(mean(h^2) + eps) per row,
  *   y = h * rstd * gain.  y and the copies are taken of the binary32 h.

@@ -371,6 +371,7 @@ def _vector(t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
 
 def _copy8(t: NVFP4Tensor, device: int) -> bytes:
     assert t.codes.get_device() == device and t.scales.get_device() == device, "a copy on the current device is wanted"
+    assert t.codes.is_contiguous() and t.scales.is_contiguous()
     assert t.codes.numel() >= t.rows * t.cols and t.scales.numel() >= t.rows * ((t.cols + 31) // 32)
     return _TENSOR_FIELDS.pack(t.codes.data_ptr(), t.scales.data_ptr(), 0, t.rows, t.cols, t.sf_layout, t.format)
 

@@ -55,6 +55,18 @@ __device__ __forceinline__ void fence_mbarrier_init() {
 // orders this thread's earlier generic-proxy accesses to shared memory before later asynchronous-proxy ones (TMA)
 __device__ __forceinline__ void fence_proxy_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// ---- clusters of ordinary CTAs: all meet, and one reads the same place of another one's shared memory ----
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_of_rank(const float* p, uint32_t rank) {
+  uint32_t at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
 // ---- programmatic dependent launch: every kernel launched with `launch_divided` or `launch_kernel` may become resident while the previous
 // kernel of the stream drains; it runs its set-up (barriers, tensor memory, descriptor prefetch) and then waits here for
 // that kernel to finish with all its writes visible.  Behind a kernel that does not know the scheme (a caller's own) the
@@ -95,6 +107,29 @@ template <typename... Params, typename... Args>
 inline cudaError_t launch_kernel(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
                                  Args&&... args) {
   return launch_divided(-1, kern, grid, block, smem, s, static_cast<Args&&>(args)...);
+}
+// `size` neighbouring CTAs along the grid's y (x where it has no y) are a cluster; as much of the SM as possible is shared memory
+template <typename... Params, typename... Args>
+inline cudaError_t launch_cluster(unsigned size, void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[3];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributePreferredSharedMemoryCarveout;
+  attr[1].val.sharedMemCarveout = 100;
+  attr[2].id = cudaLaunchAttributeClusterDimension;
+  attr[2].val.clusterDim.x = grid.y > 1 ? 1 : size;
+  attr[2].val.clusterDim.y = grid.y > 1 ? size : 1;
+  attr[2].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 3;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  return e;
 }
 constexpr int kStreamingCarveout = 7;  // an SM then has 32 KB; with 15 per cent or more it was not divided again (see quantize_rowscale.cu)
 #endif

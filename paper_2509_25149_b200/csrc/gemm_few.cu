@@ -40,17 +40,6 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float ld_of_rank(const float* p, uint32_t rank) {  // the same place of another CTA's shared memory
-  uint32_t at;
-  float v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-  return v;
-}
-
 __device__ __forceinline__ float activated(float z, int act) {
   switch (act) {
     case NVFP4_ACT_RELU2: return act_value<NVFP4_ACT_RELU2>(z);
@@ -199,24 +188,10 @@ cudaError_t launch_few(const Args& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     device_configured(configured, dev);
   }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)((a.N + kRows - 1) / kRows * a.shares));
-  cfg.blockDim = dim3(32 * kWarps);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[3];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributePreferredSharedMemoryCarveout;  // (three rings to an SM)
-  attr[1].val.sharedMemCarveout = 100;
-  attr[2].id = cudaLaunchAttributeClusterDimension;
-  attr[2].val.clusterDim.x = (unsigned)a.shares;
-  attr[2].val.clusterDim.y = attr[2].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = a.shares > 1 ? 3 : 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
-  if (e != cudaSuccess) (void)cudaGetLastError();
-  return e;
+  // (with 100 % of the SM as shared memory it has room for three rings)
+  const dim3 grid((unsigned)((a.N + kRows - 1) / kRows * a.shares));
+  return a.shares > 1 ? launch_cluster((unsigned)a.shares, kern, grid, dim3(32 * kWarps), smem, s, a)
+                      : launch_divided(100, kern, grid, dim3(32 * kWarps), smem, s, a);
 }
 
 }  // namespace

@@ -115,6 +115,25 @@ def test_product_with_an_epilogue():
     assert B._EPILOGUE_FIELDS.size == 56
 
 
+def test_the_epilogue_struct_is_packed_as_a_c_compiler_lays_it_out(tmp_path):
+    import os
+    import subprocess
+    import sys
+    src = tmp_path / "layout.c"
+    src.write_text("""#include "nvfp4.h"
+#include <stdio.h>
+#define AT(f) (int)offsetof(nvfp4_epilogue, f)
+int main(void) { printf("%d %d %d %d %d %d %d %d %d", (int)sizeof(nvfp4_epilogue), AT(bias), AT(residual), AT(ldr), AT(z_bf16), AT(ldz), AT(z8),
+                        AT(act), AT(reserved)); return 0; }
+""")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(root, "include"), str(src), "-o", str(tmp_path / "layout")], check=True)
+    said = [int(v) for v in subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout.split()]
+    packed = B._EPILOGUE_FIELDS.pack(1, 2, 3, 4, 5, 6, 7, 8)
+    assert said[0] == len(packed)
+    assert [int.from_bytes(packed[o:o + 4], sys.byteorder) for o in said[1:]] == [1, 2, 3, 4, 5, 6, 7, 8]
+
+
 def act_bwd(da=FAKE, ldda=128, z=FAKE, ldz=128, z8=None, act=1, rows=64, cols=128, dz=FAKE, lddz=128, a=FAKE, lda=128, dbias=FAKE, acc=0, ws=FAKE,
             nws=1 << 30):
     return B.lib().nvfp4_act_bwd(da, ldda, z, ldz, z8, act, rows, cols, dz, lddz, a, lda, dbias, acc, ws, nws, None)

@@ -305,6 +305,37 @@ def test_far_arguments_of_the_activations():
         R.assert_within(R.f64(a), value, (BF16 + 256 * U) * np.abs(value) + 2.0 ** -110, act)
 
 
+def test_more_than_two_to_the_31_elements():
+    rows, cols = 131080, 16392
+    at = [0, 5, rows // 2, rows - 1]
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    x[at] = normal((len(at), cols), 95).cuda()
+    x8 = B.alloc_tensor(rows, cols, format=B.FORMAT_MXFP8)
+    B.nvfp4_quantize(x, B.quant_opts(), x8)
+    y, rstd = torch.empty_like(x), torch.empty(rows, device="cuda")
+    B.nvfp4_rmsnorm_fwd(x, None, 1e-5, y, rstd)
+    h64, r64, y64 = norm64(x[at].cpu(), None, None, 1e-5)
+    R.assert_within(R.f64(y[at]), y64, np.abs(y64) * (BF16 + 2.0 ** -16) + 1e-38, "y")
+    # its gradient from the copy, with y for dy (rows of zeros leave rows of zeros)
+    dgain, ws = torch.empty(cols, device="cuda"), torch.empty(B.nvfp4_rmsnorm_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    dh = x  # (x has served)
+    B.nvfp4_rmsnorm_bwd(y, x8, None, rstd, dh, dgain, ws)
+    r, n = R.f64(rstd[at])[:, None], R.decode8(x8.codes[at].cpu().numpy(), x8.scales[at].cpu().numpy()) * R.f64(rstd[at])[:, None]
+    g = R.f64(y[at])
+    c = (g * n).mean(1, keepdims=True)
+    want = r * (g - n * c)
+    tol = r * (8 * U * (np.abs(g) + np.abs(n * c)) + np.abs(n) * 2.0 ** -17 * np.abs(g * n).mean(1, keepdims=True)) + np.abs(want) * BF16 + 1e-40
+    R.assert_within(R.f64(dh[at]), want, tol, "dh")
+    R.assert_within(R.f64(dgain), (g * n).sum(0), 128 * U * np.abs(g * n).sum(0) + 1e-40, "dgain")
+    assert not dh[1].any()
+    dbias, ws = torch.empty(cols, device="cuda"), torch.empty(B.nvfp4_act_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.nvfp4_act_bwd(y, x8, B.ACT_RELU2, dh, dbias=dbias, workspace=ws)
+    z = R.decode8(x8.codes[at].cpu().numpy(), x8.scales[at].cpu().numpy())
+    want = g * 2 * np.maximum(z, 0)
+    R.assert_within(R.f64(dh[at]), want, np.abs(want) * (BF16 + 4 * U), "dz")
+    R.assert_within(R.f64(dbias), want.sum(0), 128 * U * np.abs(want).sum(0), "dbias")
+
+
 # --------------------------------------------------------------------------------------------- streams and graphs ----
 def test_captured_on_another_stream_beside_each_other():
     """Two captured graphs with workspaces of their own, replayed on two streams at once, give the bits of direct calls."""

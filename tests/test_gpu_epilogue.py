@@ -25,7 +25,7 @@ def normal(shape, seed, std=1.0, dtype=torch.bfloat16):
 # few rows (up to 32: one to eight shares of k, short last blocks and steps); one CTA pair, few tiles with shared contractions, 128- and
 # 256-wide tiles, several rounds, 512-wide tiles (rows off 32 bytes)
 SHAPES = [(1, 8, 8), (1, 136, 264), (3, 520, 72), (8, 256, 2048), (9, 72, 520), (16, 2048, 4104), (17, 264, 16384), (31, 40, 40),
-          (32, 1048, 2056), (2, 20480, 264), (33, 1048, 2056), (40, 264, 128), (129, 1000, 200), (257, 520, 1088), (300, 2056, 64),
+          (32, 1048, 2056), (2, 20480, 264), (33, 1048, 2056), (40, 8, 8), (300, 24, 40), (40, 264, 128), (129, 1000, 200), (257, 520, 1088), (300, 2056, 64),
           (1000, 2504, 136), (2049, 2304, 72), (2305, 2600, 1032)]
 
 
@@ -99,6 +99,22 @@ def test_every_tile(tile, keep):
         check(300, 776, 1032, "gelu", True, keep)
     finally:
         B.nvfp4_set_gemm_tile_n(0)
+
+
+def test_outputs_of_more_than_two_to_the_31_elements():
+    M, N, K = 131080, 16392, 8
+    a, b = ints((M, K), 61, -2, 2), ints((N, K), 62, -2, 2)
+    res = torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")
+    rows = [0, 4, M // 2, M - 129, M - 1]
+    res[rows] = 3
+    z8 = B.alloc_tensor(M, N, format=B.FORMAT_MXFP8)
+    B.nvfp4_gemm_bf16_epilogue(a.cuda(), b.cuda(), res, None, B.ACT_RELU2, res, z8)
+    B.nvfp4_device_status()
+    for r in rows:
+        z = R.f64(a[r:r + 1]) @ R.f64(b).T
+        want = torch.from_numpy(np.maximum(z, 0) ** 2 + 3).to(torch.bfloat16).double().numpy()
+        assert np.array_equal(R.f64(res[r:r + 1]), want)
+        assert np.array_equal(R.decode8(z8.codes[r:r + 1].cpu().numpy(), z8.scales[r:r + 1].cpu().numpy()), R.decode8(*R.copy8(z)))
 
 
 def test_agrees_with_the_plain_product_bit_for_bit():
