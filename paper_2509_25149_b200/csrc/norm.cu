@@ -20,11 +20,21 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ float dot8(const float (&a)[8], const float (&b)[8], float s) {
+// Sums of squares of a lane, eight apart: short chains of additions round less, and do not wait for one another
+struct Squares {
+  float2 s[4] = {};
+  __device__ __forceinline__ void add(const float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s = fmaf(a[i], b[i], s);
-  return s;
-}
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = make_float2(v[2 * i], v[2 * i + 1]);
+      s[i] = fma2(p, p, s[i]);
+    }
+  }
+  __device__ __forceinline__ float sum() const {
+    const float2 t = add2(add2(s[0], s[1]), add2(s[2], s[3]));
+    return t.x + t.y;
+  }
+};
 
 struct Fwd {
   const uint16_t* x;
@@ -39,7 +49,7 @@ struct Fwd {
 };
 
 __device__ __forceinline__ float rstd_of(float sum, int64_t cols, float eps) {
-  return __frcp_rn(__fsqrt_rn(__fdiv_rn(sum, (float)cols) + eps));
+  return __frsqrt_rn(__fdiv_rn(sum, (float)cols) + eps);
 }
 
 // RES: 0 = no residual, 1 = bf16, 2 = binary32.  What follows the statistic, for one chunk.
@@ -104,13 +114,14 @@ __global__ void __launch_bounds__(32 * kWarpsOf<WPR>) rmsnorm_fwd_kernel(const F
       const int64_t chunk = lane + 32 * (seg + WPR * i);
       raw[i].load(a, row, chunk, row < a.rows && chunk < n);
     }
-    float v[KEEP][8], sum = 0.f;
+    float v[KEEP][8];
+    Squares squares;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       raw[i].sum(v[i]);
-      sum = dot8(v[i], v[i], sum);
+      squares.add(v[i]);
     }
-    sum = warp_sum(sum);
+    float sum = warp_sum(squares.sum());
     if (WPR > 1) {
       if (lane == 0) part[it & 1][warp] = sum;
       __syncthreads();
@@ -138,7 +149,7 @@ __global__ void __launch_bounds__(512) rmsnorm_fwd_long_kernel(const Fwd a) {
   griddep_launch_dependents();
   int it = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++it) {
-    float sum = 0.f;
+    Squares squares;
     for (int64_t c0 = 0; c0 < n; c0 += 2048) {
       Loaded<RES> raw[4];
 #pragma unroll
@@ -147,10 +158,10 @@ __global__ void __launch_bounds__(512) rmsnorm_fwd_long_kernel(const Fwd a) {
       for (int i = 0; i < 4; ++i) {
         float v[8];
         raw[i].sum(v);
-        sum = dot8(v, v, sum);
+        squares.add(v);
       }
     }
-    sum = warp_sum(sum);
+    float sum = warp_sum(squares.sum());
     if (lane == 0) part[it & 1][warp] = sum;
     __syncthreads();
     sum = 0.f;
