@@ -207,8 +207,8 @@ def nvfp4_quantize(x: torch.Tensor, opts: CQuantOpts, rowwise: Optional[NVFP4Ten
                    colwise: Optional[NVFP4Tensor] = None) -> None:
     assert x.is_cuda and x.dtype in (torch.bfloat16, torch.float32) and x.dim() == 2 and x.stride(1) == 1
     if x.dtype == torch.float32 and not (opts.flags & INPUT_FP32):  # a binary32 source is announced by a flag
-        opts = CQuantOpts(opts.block_rows, opts.rounding, opts.rht_rowwise, opts.rht_colwise, opts.rht_sign_mask,
-                          opts.flags | INPUT_FP32, opts.seed, opts.sr_offset, opts.rht_dim, opts.rht_sign_mask_ext)
+        opts = CQuantOpts.from_buffer_copy(opts)
+        opts.flags |= INPUT_FP32
     assert (x.dtype == torch.float32) == bool(opts.flags & INPUT_FP32)
     _check(lib().nvfp4_quantize(x.data_ptr(), x.shape[0], x.shape[1], x.stride(0), ctypes.byref(opts), _ref(rowwise),
                                 _ref(colwise), _stream()), "nvfp4_quantize")
@@ -353,19 +353,26 @@ def _device() -> int:
     return _get_device() if _get_device is not None else torch.cuda.current_device()
 
 
+def _refuse(t, what: str) -> None:
+    raise AssertionError(f"{what} on the current device is wanted, not {tuple(t.shape)} {t.dtype} with strides {t.stride()} on {t.device}")
+
+
+# (The checks are written for the host's time: a call's launch takes 3 us, and an attribute of a tensor 0.1.)
 def _matrix(t: torch.Tensor, shape, device: int, dtypes=_BF16) -> int:
     """Checks a row-major matrix on the current device and returns its leading dimension."""
-    stride = t.stride()
-    assert t.get_device() == device and t.dtype in dtypes and t.shape == shape and len(stride) == 2 and stride[1] == 1, \
-        f"a row-major {tuple(shape)} matrix of {dtypes} on the current device is wanted, not {tuple(t.shape)} {t.dtype} on {t.device}"
-    return stride[0] if shape[0] > 1 else shape[1]  # (a single row's stride says nothing)
+    if t.shape != shape or t.dtype not in dtypes or t.get_device() != device:
+        _refuse(t, f"a row-major {tuple(shape)} matrix of {dtypes}")
+    ld, inner = t.stride()
+    if inner != 1:
+        _refuse(t, f"a row-major {tuple(shape)} matrix of {dtypes}")
+    return ld if shape[0] > 1 else shape[1]  # (a single row's stride says nothing)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
     if t is None:
         return None
-    assert t.get_device() == device and t.dtype == torch.float32 and t.shape == (n,) and (n == 1 or t.stride(0) == 1), \
-        f"a binary32 vector of {n} on the current device is wanted, not {tuple(t.shape)} {t.dtype} on {t.device}"
+    if t.dtype is not torch.float32 or t.numel() != n or t.dim() != 1 or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, f"a binary32 vector of {n}")
     return t.data_ptr()
 
 
