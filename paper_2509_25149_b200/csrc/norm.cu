@@ -266,7 +266,7 @@ __device__ __forceinline__ void store_dh(const Bwd& a, const float2 (&g)[4], con
 // their way into a ring of ST rows in shared memory, in which every thread has places of its own (so that no group waits for another,
 // and a thread only for its own copies); so is the residual path's gradient where there is room, else it is loaded when its row's turn
 // begins.
-// A lane keeps the sums of its columns in registers over all its rows; at the end the groups add theirs in their order.
+// A lane keeps the sums of its columns in registers over all its rows; at the end those of the groups are added in their order.
 template <int H, bool F32, int WPR, int KEEP>
 struct BwdShape {
   static constexpr int kH = H == 2 ? 8 : H == 1 ? 32 : 16;  // bytes of a chunk of h
@@ -282,7 +282,7 @@ struct BwdShape {
   static constexpr int kStage = KEEP * (16 + kH + kRg) * kThreads;
   static constexpr int ST = fit(16 + kH + kRg) > 4 ? 4 : fit(16 + kH + kRg);
   static constexpr int kBytes = ST * kStage + kGain;
-  static_assert(ST >= 1 && 32 * WPR * KEEP * 32 <= ST * kStage, "the column sums reuse the ring");
+  static_assert(ST >= 1 && kGroups * 32 * WPR * KEEP * 32 <= ST * kStage, "the column sums reuse the ring");
 };
 
 template <int H, bool F32, int WPR, int KEEP>
@@ -431,27 +431,21 @@ __global__ void __launch_bounds__(BwdShape<H, F32, WPR, KEEP>::kThreads, 1) rmsn
   copy_wait<0>();
   if (!a.partial) return;
   __syncthreads();  // the ring is empty; the sums take its place
-  float* const out = a.partial + (int64_t)blockIdx.x * a.cols;
-  const int64_t left = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // (few rows: not every group had one)
-  const int last = (int)(left < kGroups ? left : kGroups) - 1;
-  for (int g = 0; g <= last; ++g) {
-    if (g == group) {
+  constexpr int kWidth = 32 * WPR * KEEP * 8;  // columns that a group has lanes for
 #pragma unroll
-      for (int i = 0; i < KEEP; ++i) {
-        const int chunk = chunk_of(i);
-        if (chunk >= n8) continue;
-        if (g > 0) {
-          const float4* const p = reinterpret_cast<const float4*>(columns + chunk * 8);
-          const float4 u = p[0], v = p[1];
-          acc[i][0] = add2(acc[i][0], make_float2(u.x, u.y));
-          acc[i][1] = add2(acc[i][1], make_float2(u.z, u.w));
-          acc[i][2] = add2(acc[i][2], make_float2(v.x, v.y));
-          acc[i][3] = add2(acc[i][3], make_float2(v.z, v.w));
-        }
-        store8<true>(g == last ? out : columns, chunk * 8, acc[i]);
-      }
+  for (int i = 0; i < KEEP; ++i)
+    if (chunk_of(i) < n8) store8<true>(columns, group * kWidth + chunk_of(i) * 8, acc[i]);
+  __syncthreads();
+  const int64_t left = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;  // (few rows: not every group had one)
+  const int groups = (int)(left < kGroups ? left : kGroups);
+  float* const out = a.partial + (int64_t)blockIdx.x * a.cols;
+  for (int c = threadIdx.x * 4; c < n8 * 8; c += T * 4) {
+    float4 t = *reinterpret_cast<const float4*>(columns + c);
+    for (int g = 1; g < groups; ++g) {
+      const float4 u = *reinterpret_cast<const float4*>(columns + g * kWidth + c);
+      t = make_float4(t.x + u.x, t.y + u.y, t.z + u.z, t.w + u.w);
     }
-    if (g < last) __syncthreads();
+    *reinterpret_cast<float4*>(out + c) = t;
   }
 }
 
