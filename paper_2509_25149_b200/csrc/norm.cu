@@ -236,10 +236,12 @@ struct LoadedH {
   }
   __device__ __forceinline__ void normalised(float rstd, float2 (&n)[4]) const {
     if (H == 2) {
-      decode8(codes, decode_scale8(byte), n);
-    } else {
-      values2(raw, n);
+      // The scale is a power of two, so 2^E rstd is exact and the product rounded once, as the value times rstd is.  (Below 2^-126, where 2^E
+      // rstd is cut to a multiple of 2^-149, n is below 2^-117.)
+      decode8(codes, decode_scale8(byte) * rstd, n);
+      return;
     }
+    values2(raw, n);
 #pragma unroll
     for (int i = 0; i < 4; ++i) n[i] = mul2(n[i], both(rstd));
   }
@@ -340,8 +342,9 @@ __global__ void __launch_bounds__(BwdShape<H, F32, WPR, KEEP>::kThreads, 1) rmsn
       for (int i = 0; i < KEEP; ++i)
         if (chunk_of(i) < n8) byte[i] = ldg8(a.h8.scales + row * a.h8.blocks + (chunk_of(i) >> 2));
   };
-  griddep_wait();
+  const float per_col = __frcp_rn((float)a.cols);  // (rounded twice instead of once: 2^-24 of c)
   const int64_t first = (int64_t)blockIdx.x + (int64_t)gridDim.x * group;
+  griddep_wait();
 #pragma unroll
   for (int u = 0; u < ST - 1; ++u) fetch(first + u * step, u);
   fetch_small(first);
@@ -412,7 +415,7 @@ __global__ void __launch_bounds__(BwdShape<H, F32, WPR, KEEP>::kThreads, 1) rmsn
 #pragma unroll
       for (int w = 0; w < WPR; ++w) sum += part[it & 1][group * WPR + w];
     }
-    const float c = __fdiv_rn(sum, (float)a.cols);
+    const float c = sum * per_col;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       if (chunk_of(i) >= n8) break;
