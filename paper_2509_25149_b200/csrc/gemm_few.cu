@@ -59,7 +59,16 @@ struct Ring {
   static_assert(kPart + kTotal <= kBytes, "the sums reuse the ring");
 };
 
-template <int MT, int ST>
+// 16 bytes of B: as copy_async, and with AHEAD the 256 bytes around them are asked into L2
+template <bool AHEAD>
+__device__ __forceinline__ void copy_weight(uint32_t dst, const void* src, bool live) {
+  if (AHEAD)
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+  else
+    copy_async<16>(dst, src, live);
+}
+
+template <int MT, int ST, bool AHEAD>
 __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
   using R = Ring<MT, ST>;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -91,7 +100,7 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
       const bool in = k < g.K;
       const uint32_t at = mine + slot * R::kStep;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) copy_async<16>(at + i * R::kPlane, brow[i] + (in ? k : 0), in && blive[i]);
+      for (int i = 0; i < 4; ++i) copy_weight<AHEAD>(at + i * R::kPlane, brow[i] + (in ? k : 0), in && blive[i]);
 #pragma unroll
       for (int j = 0; j < MT; ++j) copy_async<16>(at + (4 + j) * R::kPlane, arow[j] + (in ? k : 0), in && alive[j]);
     }
@@ -177,9 +186,9 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
   }
 }
 
-template <int MT, int ST>
-cudaError_t launch_few(const Args& a, cudaStream_t s) {
-  auto kern = few_rows_kernel<MT, ST>;
+template <int MT, int ST, bool AHEAD>
+cudaError_t launch_few_as(const Args& a, cudaStream_t s) {
+  auto kern = few_rows_kernel<MT, ST, AHEAD>;
   constexpr int smem = Ring<MT, ST>::kBytes;
   static std::atomic<uint64_t> configured{0};  // per instantiation and device
   int dev;
@@ -192,6 +201,16 @@ cudaError_t launch_few(const Args& a, cudaStream_t s) {
   const dim3 grid((unsigned)((a.N + kRows - 1) / kRows * a.shares));
   return a.shares > 1 ? launch_cluster((unsigned)a.shares, kern, grid, dim3(32 * kWarps), smem, s, a)
                       : launch_divided(100, kern, grid, dim3(32 * kWarps), smem, s, a);
+}
+// Asking L2 for 256 bytes at a time (4 steps of k) pays where a warp has 32 steps and more.  Without / with it, one row, weights that exceed
+// L2 together: 8192 x 16384 (128 steps) 46.3 / 44.1 us, 20480 x 5120 (40) 39.9 / 37.9, 7168 x 5120 (40) 14.7 / 13.8, 10240 x 4096 (32)
+// 18.7 / 17.6, 10240 x 2048 (16) 9.9 / 9.8, 5120 x 5120 (20) 11.6 / 12.7, 20480 x 1024 (8) 10.7 / 11.4.  With 17 rows and more the operations on
+// A weigh as much and it is even (20480 x 5120, 32 rows: 51.3 / 51.9, 8192 x 16384 70.0 / 69.0).
+template <int MT, int ST>
+cudaError_t launch_few(const Args& a, cudaStream_t s) {
+  if constexpr (MT <= 2)
+    if ((a.K + 31) / 32 >= 32 * kWarps * a.shares) return launch_few_as<MT, ST, true>(a, s);
+  return launch_few_as<MT, ST, false>(a, s);
 }
 
 }  // namespace

@@ -27,6 +27,7 @@ def normal(shape, seed, std=1.0, dtype=torch.bfloat16):
 SHAPES = [(1, 8, 8), (1, 136, 264), (3, 520, 72), (8, 256, 2048), (9, 72, 520), (16, 2048, 4104), (17, 264, 16384), (31, 40, 40),
           (32, 1048, 2056), (2, 20480, 264), (33, 1048, 2056), (40, 8, 8), (300, 24, 40), (40, 264, 128), (129, 1000, 200), (257, 520, 1088), (300, 2056, 64),
           (1000, 2504, 136), (2049, 2304, 72), (2305, 2600, 1032)]
+SHAPES += [(1, 40, 33000), (13, 72, 33000), (21, 40, 33000), (4, 7144, 4104)]  # few rows whose warps have 32 steps of k and more
 
 
 @pytest.mark.parametrize("shape", SHAPES)
