@@ -554,6 +554,8 @@ nvfp4_status nvfp4_gemm_bf16_epilogue(const void* A, int64_t lda, const void* B,
   const nvfp4_status st = epilogue_prepare(A, lda, B, ldb, M, N, K, epilogue, D_bf16, ldd, g, e);
   if (st != NVFP4_OK) return st;
   const int forced = g_tile_n.load(std::memory_order_relaxed);
+  if (!forced && gemm_tokens_pays(g, e))
+    return launch_gemm_tokens(g, e, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
   if (M <= kFewRows && !forced)
     return launch_gemm_few_rows(g, e, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? NVFP4_OK : NVFP4_ERR_CUDA;
   Bf16Wide wide;

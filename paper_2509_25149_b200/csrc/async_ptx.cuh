@@ -66,6 +66,12 @@ __device__ __forceinline__ float ld_of_rank(const float* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
+// one's own address, but in the shared memory of another CTA of the cluster
+__device__ __forceinline__ void st_of_rank(uint32_t own, uint32_t rank, uint32_t v) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(own), "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
 
 // ---- programmatic dependent launch: every kernel launched with `launch_divided` or `launch_kernel` may become resident while the previous
 // kernel of the stream drains; it runs its set-up (barriers, tensor memory, descriptor prefetch) and then waits here for

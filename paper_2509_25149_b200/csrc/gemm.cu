@@ -27,6 +27,7 @@
 #include "gemm_2cta.cuh"
 #include "gemm_wide.cuh"
 #include "gemm_bf16.cuh"
+#include "gemm_tokens.cuh"
 
 namespace nvfp4 {
 
@@ -899,6 +900,69 @@ cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs
   // more.  With the stage / with buffers: 4096 x 5120 x 512 30.9 / 25.5 us (GELU besides 41.3 / 36.3), x 1024 37.1 / 37.6 (46.1 / 42.1), x 1536
   // 50.5 / 52.4 (54.9 / 56.7), x 4096 132.3 / 133.6 (135.8 / 141.0).
   return e.residual && g.K <= 1024 ? launch_bf16_epilogue<256, 1, dense::EpilogueBuffers>(g, e, wide, pairs, s) : launch_bf16_epilogue<256>(g, e, wide, pairs, s);
+}
+
+template <int MT, int ST>
+static cudaError_t launch_tokens(const DenseGemmArgs& g, const FewArgs& a, cudaStream_t s) {
+  using C = tokens::Cfg<MT, ST>;
+  CUtensorMap map_w, map_x;
+  const CUtensorMapDataType bf = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  if (!make_map_2d(&map_w, bf, 2, g.b, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldb * 2, 64, tokens::kCols, true) ||
+      !make_map_2d(&map_x, bf, 2, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda * 2, 64, MT, true))
+    return cudaErrorInvalidValue;
+  auto kern = tokens::tokens_kernel<MT, ST>;
+  static std::atomic<uint64_t> configured{0};  // per instantiation and device
+  int dev;
+  if (device_needs_config(configured, &dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kBytes);
+    if (e != cudaSuccess) return e;
+    device_configured(configured, dev);
+  }
+  const dim3 grid((unsigned)((g.N + tokens::kCols - 1) / tokens::kCols * a.shares)), block(tokens::kThreads);
+  const cudaError_t e = a.shares > 1 ? launch_cluster((unsigned)a.shares, kern, grid, block, C::kBytes, s, map_w, map_x, a)
+                                     : launch_divided(100, kern, grid, block, C::kBytes, s, map_w, map_x, a);
+  count_launch();
+  return e;
+}
+
+// Shares of k: as many as leave all CTAs resident, two to an SM, and keep two k-blocks for each.  Clusters of three and more fill 7 of 8 places (5120
+// rows of B, 40 tiles, 5120 deep, 64 rows of A: 5 / 6 / 7 shares 15.5 / 14.7 / 22.9 us; 32 tiles, 4096 deep: 7 / 8 shares 12.4 / 11.5), clusters of
+// two all of them (136 tiles, 4096 deep: 1 / 2 shares 30.5 / 29.0).
+static int token_shares(int64_t N, int64_t K, int sms) {
+  const int64_t tiles = (N + tokens::kCols - 1) / tokens::kCols, most = std::min<int64_t>(8, (K + 63) / 64 / 2);
+  const int64_t s = std::min<int64_t>(most, std::max<int64_t>(7 * sms / (4 * tiles), tiles <= sms ? 2 : 1));
+  return s < 1 ? 1 : (int)s;
+}
+
+// Where that is faster than the few-rows kernel (up to 32 rows of A) and the pair kernels; here / there, us, weights that exceed L2 together:
+//   up to 8 rows   large weights: 20480 x 5120 35.9 / 38.4, 5120 x 20480 35.4 / 40.1, but 7168 x 5120 15.5 / 14.5, 4096 x 4096 9.9 / 8.4
+//   up to 16       5120 x 5120 12.4 / 13.7, 7168 x 5120 15.4 / 16.1, but 8192 x 2048 9.7 / 8.2, 1024 x 16384 12.9 / 11.2
+//   up to 32       2560 x 2560 7.3 / 8.2, 5120 x 5120 13.0 / 17.2, 5120 x 20480 36.3 / 57.3, but 2048 x 2048 5.7 / 5.3, 512 x 16384 12.5 / 10.8
+//   up to 64       1024 x 1024 5.4 / 6.3, 5120 x 5120 14.7 / 25.3, 5120 x 20480 39.0 / 88, 20480 x 256 6.6 / 9.4, but 512 x 512 5.8 / 5.6,
+//                  1024 x 256 7.0 / 4.6
+//   up to 128      (128 rows) 5120 x 5120 17.6 / 25.7, 5120 x 20480 42.8 / 89, 20480 x 5120 47.5 / 60.4, but 2048 x 2048 9.8 / 9.1, 8192 x 2048
+//                  14.8 / 13.2, and where 256-wide tiles are nearly a round of the pairs: 14336 x 4096 31.5 / 28.6, 16384 x 4096 33.7 / 29.6
+// (256 rows are as many bytes from L2 as two tiles of B: 5120 x 5120 26.0 / 26.1, 20480 x 5120 87 / 62.)
+// Codes of 8 bits want sums of no more than kShare k-blocks.
+bool gemm_tokens_pays(const DenseGemmArgs& g, const EpilogueArgs& e) {
+  int sms = 0;
+  if (g.M > kTokenRows || sm_count(&sms) != cudaSuccess) return false;
+  const int64_t blocks = ((int64_t)g.K + 63) / 64, weight = (int64_t)g.N * g.K;
+  if (e.z8_codes && blocks > (int64_t)dense::kShare * token_shares(g.N, g.K, sms)) return false;
+  if (g.M <= 16) return weight >= (g.M <= 8 ? 40000000 : 20000000) && g.N > 15 * tokens::kCols;
+  if (g.M <= 32) return weight >= 5000000 && g.N > 7 * tokens::kCols;
+  if (g.M <= 64) return g.K >= 1024 || g.N > (int64_t)sms * tokens::kCols;
+  const int wide = (g.N + 255) / 256, pairs = sms / 2;
+  return g.K >= 4096 && (wide > pairs || 10 * wide <= 7 * pairs);
+}
+
+cudaError_t launch_gemm_tokens(const DenseGemmArgs& g, const EpilogueArgs& e, cudaStream_t s) {
+  FewArgs a = few_args(g, e);
+  int sms = 0;
+  const cudaError_t err = sm_count(&sms);
+  if (err != cudaSuccess) return err;
+  a.shares = token_shares(g.N, g.K, sms);
+  return g.M <= 32 ? launch_tokens<32, 5>(g, a, s) : g.M <= 64 ? launch_tokens<64, 4>(g, a, s) : launch_tokens<128, 3>(g, a, s);
 }
 
 // Test aid: one warp waits, with the given limit, on a barrier nobody arrives at.  The wait runs out, the code lands

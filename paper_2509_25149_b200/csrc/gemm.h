@@ -92,6 +92,10 @@ cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs
 // the same for at most kFewRows rows of A (gemm_few.cu)
 constexpr int kFewRows = 32;
 cudaError_t launch_gemm_few_rows(const DenseGemmArgs& g, const EpilogueArgs& e, cudaStream_t s);
+// and for at most kTokenRows (gemm_tokens.cuh)
+constexpr int kTokenRows = 128;
+bool gemm_tokens_pays(const DenseGemmArgs& g, const EpilogueArgs& e);
+cudaError_t launch_gemm_tokens(const DenseGemmArgs& g, const EpilogueArgs& e, cudaStream_t s);
 cudaError_t launch_gemm_bf16(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, const Bf16Wide& wide, cudaStream_t s);
 
 }  // namespace nvfp4

@@ -1,16 +1,13 @@
 // BF16 product of a few rows (tokens in generation) with a weight, and its epilogue:  z = A B^T + bias, D = act(z) + residual.
 // Bound by the bytes of the weight B [N x K]: 2 flops per byte and row.  The tensor-memory kernels work on 256 rows at a time and take
-// as long for one row as for 256 (1 x 5120 x 5120 31 us); here B streams from memory straight into the registers of warp-wide
+// as long for one row as for 256 (1 x 5120 x 5120 31 us), and those of gemm_tokens.cuh start slower (8 x 5120 x 5120 12.3 us, here 11.7); here B streams from memory straight into the registers of warp-wide
 // mma.sync instructions, 16 rows of B against 8 rows of A.  The order of k within an instruction is free as long as both operands agree: a lane
 // takes 16 neighbouring bytes of a row of B and the same 16 bytes of a row of A, and they are its fragments of two instructions, without
 // shuffles.  They come by cp.async through a ring in shared memory that belongs to the thread alone, so that the steps to come are always
 // in flight and nobody waits for anybody.
 // A CTA has 32 rows of B (a block of the copy in 8 bits), its four warps a share of k each; where that leaves too few CTAs, a cluster
 // of up to eight shares k once more.  Partial sums are added in the order of the shares: the same bits in every run.
-#include "act.cuh"
-#include "around.h"
-#include "copy8.cuh"
-#include "gemm.h"
+#include "few.cuh"
 
 namespace nvfp4 {
 
@@ -18,37 +15,11 @@ namespace {
 
 constexpr int kWarps = 4, kRows = 32;  // of B
 
-struct Args {
-  const uint16_t* a;
-  const uint16_t* b;
-  uint16_t* d;
-  const float* bias;
-  const uint16_t* residual;
-  uint16_t* z;
-  Copy8 z8;
-  int64_t lda, ldb, ldd, ldr, ldz;
-  int M, N, K, act, shares;  // shares: CTAs of a cluster
-};
-
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ float activated(float z, int act) {
-  switch (act) {
-    case NVFP4_ACT_RELU2: return act_value<NVFP4_ACT_RELU2>(z);
-    case NVFP4_ACT_SILU: return act_value<NVFP4_ACT_SILU>(z);
-    case NVFP4_ACT_GELU: return act_value<NVFP4_ACT_GELU>(z);
-    default: return z;
-  }
-}
-
 // MT: groups of eight rows of A;  ST: steps of 32 k that the ring has room for
 template <int MT, int ST>
 struct Ring {
@@ -59,17 +30,8 @@ struct Ring {
   static_assert(kPart + kTotal <= kBytes, "the sums reuse the ring");
 };
 
-// 16 bytes of B: as copy_async, and with AHEAD the 256 bytes around them are asked into L2
-template <bool AHEAD>
-__device__ __forceinline__ void copy_weight(uint32_t dst, const void* src, bool live) {
-  if (AHEAD)
-    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-  else
-    copy_async<16>(dst, src, live);
-}
-
-template <int MT, int ST, bool AHEAD>
-__global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
+template <int MT, int ST>
+__global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) {
   using R = Ring<MT, ST>;
   extern __shared__ __align__(16) uint8_t smem[];
   auto part = reinterpret_cast<float(*)[8 * MT][kRows + 1]>(smem);      // [warp][row of A][row of B]
@@ -100,13 +62,17 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
       const bool in = k < g.K;
       const uint32_t at = mine + slot * R::kStep;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) copy_weight<AHEAD>(at + i * R::kPlane, brow[i] + (in ? k : 0), in && blive[i]);
+      for (int i = 0; i < 4; ++i) copy_async<16>(at + i * R::kPlane, brow[i] + (in ? k : 0), in && blive[i]);
 #pragma unroll
       for (int j = 0; j < MT; ++j) copy_async<16>(at + (4 + j) * R::kPlane, arow[j] + (in ? k : 0), in && alive[j]);
     }
     copy_commit();  // (an empty group where there is no step: the count of groups stays that of the steps)
   };
   griddep_wait();
+  constexpr int kOwn = 8 * MT / kWarps;
+  const float bias = bias_of(g, n0 + lane);
+  float res[kOwn] = {};
+  residual_rows(g, res, n0 + lane, warp, kWarps);
 #pragma unroll
   for (int u = 0; u < ST - 1; ++u) fetch(s0 + u, u);
   float acc[2][MT][4] = {};
@@ -143,7 +109,6 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
       for (int e = 0; e < 4; ++e) part[warp][8 * j + 2 * t + (e & 1)][16 * r + gid + 8 * (e >> 1)] = acc[r][j][e];
   __syncthreads();
   // a warp to a row of A from here on (rows warp, warp + 4, ...), a lane to a column of D
-  constexpr int kOwn = 8 * MT / kWarps;
   float v[kOwn];
 #pragma unroll
   for (int j = 0; j < kOwn; ++j) {
@@ -162,33 +127,12 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const Args g) {
     cluster_sync();  // none may go while its sums are read
     if (rank != 0) return;
   }
-  const int n = n0 + lane;
-  const bool live = n < g.N;
-  const float bias = g.bias && live ? g.bias[n] : 0.f;
-#pragma unroll
-  for (int j = 0; j < kOwn; ++j) {
-    const int64_t m = kWarps * j + warp;
-    if (m >= g.M) break;  // (the same for the whole warp)
-    const float z = v[j] + bias;
-    if (g.z8.codes) {
-      float top = live ? fabsf(z) : 0.f;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const uint32_t byte = scale_byte8(top);
-      if (live) g.z8.codes[m * g.N + n] = (uint8_t)e4m3x4(z * encode_scale8(byte), 0.f, 0.f, 0.f);
-      if (lane == 0) g.z8.scales[m * g.z8.blocks + (n0 >> 5)] = (uint8_t)byte;
-    }
-    if (!live) continue;
-    if (g.z) g.z[m * g.ldz + n] = (uint16_t)pack2(z, 0.f);
-    float d = activated(z, g.act);
-    if (g.residual) d += bf16_lo(g.residual[m * g.ldr + n]);
-    g.d[m * g.ldd + n] = (uint16_t)pack2(d, 0.f);
-  }
+  finish_rows<kOwn>(g, v, res, bias, n0, warp, kWarps, lane);
 }
 
-template <int MT, int ST, bool AHEAD>
-cudaError_t launch_few_as(const Args& a, cudaStream_t s) {
-  auto kern = few_rows_kernel<MT, ST, AHEAD>;
+template <int MT, int ST>
+cudaError_t launch_few(const FewArgs& a, cudaStream_t s) {
+  auto kern = few_rows_kernel<MT, ST>;
   constexpr int smem = Ring<MT, ST>::kBytes;
   static std::atomic<uint64_t> configured{0};  // per instantiation and device
   int dev;
@@ -202,31 +146,10 @@ cudaError_t launch_few_as(const Args& a, cudaStream_t s) {
   return a.shares > 1 ? launch_cluster((unsigned)a.shares, kern, grid, dim3(32 * kWarps), smem, s, a)
                       : launch_divided(100, kern, grid, dim3(32 * kWarps), smem, s, a);
 }
-// Asking L2 for 256 bytes at a time (4 steps of k) pays where a warp has 32 steps and more.  Without / with it, one row, weights that exceed
-// L2 together: 8192 x 16384 (128 steps) 46.3 / 44.1 us, 20480 x 5120 (40) 39.9 / 37.9, 7168 x 5120 (40) 14.7 / 13.8, 10240 x 4096 (32)
-// 18.7 / 17.6, 10240 x 2048 (16) 9.9 / 9.8, 5120 x 5120 (20) 11.6 / 12.7, 20480 x 1024 (8) 10.7 / 11.4.  With 17 rows and more the operations on
-// A weigh as much and it is even (20480 x 5120, 32 rows: 51.3 / 51.9, 8192 x 16384 70.0 / 69.0).
-template <int MT, int ST>
-cudaError_t launch_few(const Args& a, cudaStream_t s) {
-  if constexpr (MT <= 2)
-    if ((a.K + 31) / 32 >= 32 * kWarps * a.shares) return launch_few_as<MT, ST, true>(a, s);
-  return launch_few_as<MT, ST, false>(a, s);
-}
-
 }  // namespace
 
 cudaError_t launch_gemm_few_rows(const DenseGemmArgs& g, const EpilogueArgs& e, cudaStream_t s) {
-  Args a{};
-  a.a = static_cast<const uint16_t*>(g.a);
-  a.b = static_cast<const uint16_t*>(g.b);
-  a.d = static_cast<uint16_t*>(g.d);
-  a.bias = e.bias;
-  a.residual = static_cast<const uint16_t*>(e.residual);
-  a.z = static_cast<uint16_t*>(e.z);
-  a.z8 = Copy8{e.z8_codes, e.z8_scales, blocks8(g.N)};
-  a.lda = g.lda; a.ldb = g.ldb; a.ldd = g.ldd; a.ldr = e.ldr; a.ldz = e.ldz;
-  a.M = g.M; a.N = g.N; a.K = g.K;
-  a.act = e.act;
+  FewArgs a = few_args(g, e);
   int sms = 0;
   const cudaError_t err = sm_count(&sms);
   if (err != cudaSuccess) return err;

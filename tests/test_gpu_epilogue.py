@@ -27,7 +27,10 @@ def normal(shape, seed, std=1.0, dtype=torch.bfloat16):
 SHAPES = [(1, 8, 8), (1, 136, 264), (3, 520, 72), (8, 256, 2048), (9, 72, 520), (16, 2048, 4104), (17, 264, 16384), (31, 40, 40),
           (32, 1048, 2056), (2, 20480, 264), (33, 1048, 2056), (40, 8, 8), (300, 24, 40), (40, 264, 128), (129, 1000, 200), (257, 520, 1088), (300, 2056, 64),
           (1000, 2504, 136), (2049, 2304, 72), (2305, 2600, 1032)]
-SHAPES += [(1, 40, 33000), (13, 72, 33000), (21, 40, 33000), (4, 7144, 4104)]  # few rows whose warps have 32 steps of k and more
+SHAPES += [(1, 40, 33000), (13, 72, 33000), (21, 40, 33000), (4, 7144, 4104)]  # few rows, long contractions
+# up to 128 rows: every width of tile with and without shares of k, short last tiles and k-blocks, one CTA and a full chip
+SHAPES += [(3, 10248, 4104), (12, 5128, 4104), (16, 2056, 10248), (20, 2568, 2056), (32, 1000, 5320), (33, 8, 1024), (50, 19208, 72), (57, 1160, 1096),
+           (64, 264, 16392), (64, 5000, 1032), (65, 392, 4104), (100, 2600, 4360), (128, 5128, 4104), (128, 8, 8200)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -90,6 +93,29 @@ def test_random_data(shape, act):
     check(*shape, act, True, "bf16")
     check(*shape, act, False, "8")
     check(*shape, act, True, None, bias=False, std=3.0)
+
+
+@pytest.mark.parametrize("shape", [(10, 2568, 8200), (30, 2056, 2568), (48, 1032, 4104), (64, 520, 2056), (90, 392, 8200), (120, 2056, 4104)])
+@pytest.mark.parametrize("act", sorted(R.ACTS))
+def test_random_data_of_some_tens_of_rows(shape, act):
+    check(*shape, act, True, "bf16")
+    check(*shape, act, False, "8")
+    check(*shape, act, True, None, bias=False, std=3.0)
+
+
+def test_more_tiles_than_share_a_contraction():
+    check(66, 19080, 4104, "silu", True, "bf16")
+
+
+def test_residual_in_place():
+    """D may be the residual: each element is read by the thread that writes it."""
+    for M, N, K in [(5, 520, 264), (20, 2568, 2056), (40, 1032, 1096), (60, 19208, 72), (128, 2056, 4104), (300, 520, 264)]:
+        a, b, res = ints((M, K), 21, -1, 1), ints((N, K), 22, -1, 1), ints((M, N), 23, -60, 60)
+        D = res.cuda()
+        B.nvfp4_gemm_bf16_epilogue(a.cuda(), b.cuda(), D, residual=D)
+        B.nvfp4_device_status()
+        want = R.f64(a) @ R.f64(b).T + R.f64(res)
+        assert np.array_equal(R.f64(D), torch.from_numpy(want).to(torch.bfloat16).double().numpy()), (M, N, K)
 
 
 @pytest.mark.parametrize("tile", [512, 640, 642, 644])
