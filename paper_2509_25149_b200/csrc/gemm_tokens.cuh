@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = g.shares > 1 ? (int)cluster_rank() : 0;
   const int n0 = (int)(blockIdx.x / (unsigned)g.shares) * kCols;
-  const int blocks = (g.K + 63) / 64;
+  const int blocks = (g.K + 63) / 64, tiles = (g.N + kCols - 1) / kCols;
   const int k0 = (int)((int64_t)blocks * rank / g.shares), k1 = (int)((int64_t)blocks * (rank + 1) / g.shares);  // (never empty: see the launch)
 
   if (threadIdx.x == 0) {
@@ -95,12 +95,16 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
   if (warp == 0 && lane == 0) {
     int stage = 0;
     uint32_t phase = 0;
-    for (int kb = k0; kb < k1; ++kb) {
+    // With few rows of A all CTAs would want the same few lines of it from L2 at the same time, so each begins somewhere else: 20480 x 5120, one row
+    // 45.2 us without, 35.3 with; 16 rows 35.6 / 36.1.
+    int kb = g.M <= 8 ? k0 + (int)((int64_t)(k1 - k0) * (n0 / kCols) / tiles) : k0;
+    for (int left = k1 - k0; left > 0; --left) {
       if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, 0xF00u + stage)) break;
       const uint32_t st = base + stage * C::kStage;
       mbar_expect_tx(full_bar(stage), C::kStage);  // (rows and k that are not there count: they come as zeros)
       tma_load_2d(st, &map_w, kb * 64, n0, full_bar(stage));
       tma_load_2d(st + kCols * 128, &map_x, kb * 64, 0, full_bar(stage));
+      if (++kb == k1) kb = k0;
       if (++stage == ST) {
         stage = 0;
         phase ^= 1u;
