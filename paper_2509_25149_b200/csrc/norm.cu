@@ -15,10 +15,18 @@ namespace nvfp4 {
 
 namespace {
 
-__device__ __forceinline__ float warp_sum(float v) {
+template <class T>
+__device__ __forceinline__ T warp_sum(T v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+template <int N>
+__device__ __forceinline__ double sum_of(const double* part) {
+  double s[4] = {};
+#pragma unroll
+  for (int w = 0; w < N; ++w) s[w & 3] += part[w];
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 // Sums of squares of a lane, eight apart: short chains of additions round less, and do not wait for one another
 struct Squares {
@@ -48,13 +56,24 @@ struct Fwd {
   float eps;
 };
 
-__device__ __forceinline__ float rstd_of(float sum, int64_t cols, float eps) {
-  return __frsqrt_rn(__fdiv_rn(sum, (float)cols) + eps);
+// 1 / sqrt(mean + eps) as the sum of two floats: a value in binary32, e off by some 2^-23 of itself, and one step of Newton's method in 64 bits,
+// which leaves 1.5 e^2.  The copy of y in 8 bits wants it: of its codes those come out a step off whose y crosses a border by its error, and with
+// the root and both products rounded to 24 bits they were twice as many.  (8192 x 5120 with the copy 61.3 -> 61.8 us, 16384 x 256 8.7 -> 7.8, 2048 x 20480 64.6 ->
+// 67.0: mean and root in binary32 took divisions and roots of their own.)
+struct Rstd {
+  float hi, lo;
+};
+__device__ __forceinline__ Rstd rstd_of(double sum, double per_col, float eps) {
+  const double m = fma(sum, per_col, (double)eps);
+  const double y = (double)rsqrtf((float)m);
+  const double r = y > 0. ? fma(0.5 * y, fma(-m * y, y, 1.), y) : y;  // (squares beyond binary32: y is 0)
+  const float hi = (float)r;
+  return {hi, (float)(r - (double)hi)};
 }
 
 // RES: 0 = no residual, 1 = bf16, 2 = binary32.  What follows the statistic, for one chunk.
 template <int RES>
-__device__ __forceinline__ void finish_chunk(const Fwd& a, const float (&v)[8], float rstd, int64_t row, int64_t chunk, bool live) {
+__device__ __forceinline__ void finish_chunk(const Fwd& a, const float (&v)[8], const Rstd& rstd, int64_t row, int64_t chunk, bool live) {
   if (RES && a.h && live) store8<RES == 2>(a.h, row * a.ldh + chunk * 8, v);
   if (a.h8.codes) store_chunk8(a.h8, v, row, chunk, a.cols, live);
   if (!a.y && !a.y8.codes) return;
@@ -62,7 +81,13 @@ __device__ __forceinline__ void finish_chunk(const Fwd& a, const float (&v)[8], 
   if (live) {
     load_gain(a.gain, chunk * 8, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = v[i] * rstd * g[i];
+    for (int i = 0; i < 8; i += 2) {  // v (hi + lo) g, rounded once
+      const float2 w = make_float2(v[i], v[i + 1]), gain = make_float2(g[i], g[i + 1]), n = mul2(w, both(rstd.hi));
+      const float2 off = fma2(w, both(rstd.lo), fma2(w, both(rstd.hi), make_float2(-n.x, -n.y)));
+      const float2 t = fma2(n, gain, mul2(off, gain));
+      y[i] = t.x;
+      y[i + 1] = t.y;
+    }
     if (a.y) store8<false>(a.y, row * a.ldy + chunk * 8, y);
   }
   if (a.y8.codes) store_chunk8(a.y8, y, row, chunk, a.cols, live);
@@ -96,12 +121,14 @@ template <int WPR>
 constexpr int kWarpsOf = WPR < 4 ? 4 : WPR;  // warps of a CTA
 
 // WPR warps to a row, whose lanes take every WPR-th group of 32 chunks
+// (64 registers hold a row's values but for binary32 residuals of the longest rows; one more costs an eighth of the warps)
 template <int RES, int WPR, int KEEP>
-__global__ void __launch_bounds__(32 * kWarpsOf<WPR>) rmsnorm_fwd_kernel(const Fwd a) {
+__global__ void __launch_bounds__(32 * kWarpsOf<WPR>, RES == 2 && WPR > 4 ? 1 : 32 / kWarpsOf<WPR>) rmsnorm_fwd_kernel(const Fwd a) {
   constexpr int kWarps = kWarpsOf<WPR>, kRows = kWarps / WPR;
-  __shared__ float part[2][kWarps];
+  __shared__ double part[2][kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, seg = warp % WPR, sub = warp / WPR;
   const int64_t n = a.cols >> 3;
+  const double per_col = 1. / (double)a.cols;
   griddep_wait();
   griddep_launch_dependents();
   int it = 0;
@@ -121,16 +148,14 @@ __global__ void __launch_bounds__(32 * kWarpsOf<WPR>) rmsnorm_fwd_kernel(const F
       raw[i].sum(v[i]);
       squares.add(v[i]);
     }
-    float sum = warp_sum(squares.sum());
+    double sum = warp_sum((double)squares.sum());
     if (WPR > 1) {
       if (lane == 0) part[it & 1][warp] = sum;
       __syncthreads();
-      sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < WPR; ++w) sum += part[it & 1][sub * WPR + w];
+      sum = sum_of<WPR>(part[it & 1] + sub * WPR);
     }
-    const float rstd = rstd_of(sum, a.cols, a.eps);
-    if (a.rstd && seg == 0 && lane == 0 && row < a.rows) a.rstd[row] = rstd;
+    const Rstd rstd = rstd_of(sum, per_col, a.eps);
+    if (a.rstd && seg == 0 && lane == 0 && row < a.rows) a.rstd[row] = rstd.hi;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
       const int64_t chunk = lane + 32 * (seg + WPR * i);
@@ -142,9 +167,10 @@ __global__ void __launch_bounds__(32 * kWarpsOf<WPR>) rmsnorm_fwd_kernel(const F
 // Longer rows: a CTA to a row, which is read twice (the second time from L2)
 template <int RES>
 __global__ void __launch_bounds__(512) rmsnorm_fwd_long_kernel(const Fwd a) {
-  __shared__ float part[2][16];
+  __shared__ double part[2][16];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t n = a.cols >> 3;
+  const double per_col = 1. / (double)a.cols;
   griddep_wait();
   griddep_launch_dependents();
   int it = 0;
@@ -161,14 +187,12 @@ __global__ void __launch_bounds__(512) rmsnorm_fwd_long_kernel(const Fwd a) {
         squares.add(v);
       }
     }
-    float sum = warp_sum(squares.sum());
+    double sum = warp_sum((double)squares.sum());
     if (lane == 0) part[it & 1][warp] = sum;
     __syncthreads();
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) sum += part[it & 1][w];
-    const float rstd = rstd_of(sum, a.cols, a.eps);
-    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+    sum = sum_of<16>(part[it & 1]);
+    const Rstd rstd = rstd_of(sum, per_col, a.eps);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd.hi;
     for (int64_t c0 = 0; c0 < n; c0 += 1024) {
       Loaded<RES> raw[2];
 #pragma unroll
