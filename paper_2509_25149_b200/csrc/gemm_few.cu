@@ -30,7 +30,12 @@ struct Ring {
   static_assert(kPart + kTotal <= kBytes, "the sums reuse the ring");
 };
 
-template <int MT, int ST>
+// SHARES: an accumulator takes no more than kShareSteps steps, 1024 products, and is then added to sums in registers, rounded to nearest: what
+// the instructions cut off grows with the length of a chain, and codes of 8 bits show it (65536 products of one sign in four chains, each a
+// warp's: 7.6e-5 of the sum off, in shares 8.7e-7).  For calls that keep z in 8 bits and whose chains would be longer: one row x 5120 x 20480
+// 41.9 / 42.7 us, 16 rows 49.5 / 50.3, 32 x 16384 x 16384 120 / 127 (the whole sum / in shares; the registers of the second set of sums).
+constexpr int kShareSteps = 32;
+template <int MT, int ST, bool SHARES>
 __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) {
   using R = Ring<MT, ST>;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -75,9 +80,18 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) 
   residual_rows(g, res, n0 + lane, warp, kWarps);
 #pragma unroll
   for (int u = 0; u < ST - 1; ++u) fetch(s0 + u, u);
-  float acc[2][MT][4] = {};
-  int slot = 0, next = ST - 1;
+  float acc[2][MT][4] = {}, sums[SHARES ? 2 : 1][SHARES ? MT : 1][4] = {};
+  int slot = 0, next = ST - 1, until = s0 + kShareSteps;
   for (int s = s0; s < s1; ++s) {
+    if (SHARES && s == until) {
+      until += kShareSteps;
+#pragma unroll
+      for (int i = 0; i < 8 * MT; ++i) {
+        float& a = acc[i / (4 * MT)][i / 4 % MT][i % 4];
+        sums[SHARES ? i / (4 * MT) : 0][SHARES ? i / 4 % MT : 0][i % 4] += a;
+        a = 0.f;
+      }
+    }
     copy_wait<ST - 2>();
     const uint32_t at = mine + slot * R::kStep;
     uint4 b[4], a[MT];
@@ -106,7 +120,8 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) 
 #pragma unroll
     for (int j = 0; j < MT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) part[warp][8 * j + 2 * t + (e & 1)][16 * r + gid + 8 * (e >> 1)] = acc[r][j][e];
+      for (int e = 0; e < 4; ++e) part[warp][8 * j + 2 * t + (e & 1)][16 * r + gid + 8 * (e >> 1)] =
+            SHARES ? sums[SHARES ? r : 0][SHARES ? j : 0][e] + acc[r][j][e] : acc[r][j][e];
   __syncthreads();
   // a warp to a row of A from here on (rows warp, warp + 4, ...), a lane to a column of D
   float v[kOwn];
@@ -130,9 +145,9 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) 
   finish_rows<kOwn>(g, v, res, bias, n0, warp, kWarps, lane);
 }
 
-template <int MT, int ST>
+template <int MT, int ST, bool SHARES>
 cudaError_t launch_few(const FewArgs& a, cudaStream_t s) {
-  auto kern = few_rows_kernel<MT, ST>;
+  auto kern = few_rows_kernel<MT, ST, SHARES>;
   constexpr int smem = Ring<MT, ST>::kBytes;
   static std::atomic<uint64_t> configured{0};  // per instantiation and device
   int dev;
@@ -145,6 +160,11 @@ cudaError_t launch_few(const FewArgs& a, cudaStream_t s) {
   const dim3 grid((unsigned)((a.N + kRows - 1) / kRows * a.shares));
   return a.shares > 1 ? launch_cluster((unsigned)a.shares, kern, grid, dim3(32 * kWarps), smem, s, a)
                       : launch_divided(100, kern, grid, dim3(32 * kWarps), smem, s, a);
+}
+template <int MT, int ST>
+cudaError_t launch_few(const FewArgs& a, cudaStream_t s) {
+  const int steps = (a.K + 31) / 32, warps = kWarps * a.shares;
+  return a.z8.codes && steps > kShareSteps * warps ? launch_few<MT, ST, true>(a, s) : launch_few<MT, ST, false>(a, s);
 }
 }  // namespace
 
