@@ -40,10 +40,11 @@ __device__ __forceinline__ float act_slope(float z, float& value) {
     return fmaf(value, 1.f - s, s);
   }
   if (ACT == NVFP4_ACT_GELU) {
-    const float zz = z * z;
-    const float s = logistic(kGelu2c * z * fmaf(kGelu3, zz, 1.f));
+    // (beyond |z| = 100 s is 0 or 1 and the second term zero: its factor must not be infinite there)
+    const float zz = fminf(z * z, 1e4f);
+    const float s = logistic(z * fmaf(kGelu2c * kGelu3, zz, kGelu2c));
     value = z * s;
-    return fmaf(value * (1.f - s), kGelu2c * fmaf(3.f * kGelu3, zz, 1.f), s);
+    return fmaf(value * (1.f - s), fmaf(3.f * kGelu2c * kGelu3, zz, kGelu2c), s);
   }
   value = z;
   return 1.f;

@@ -1,4 +1,5 @@
-"""Where the operators around the linear layers have little room: long contractions whose codes must not show how the tensor cores add."""
+"""Where the operators around the linear layers have little room: long contractions whose codes must not show how the tensor cores add,
+and finite arguments whose squares are beyond binary32."""
 import numpy as np
 import pytest
 import torch
@@ -46,3 +47,24 @@ def test_codes_of_long_contractions_of_one_sign(M, N, tile):
     # (an element's own half step, or half the smallest step of its block, 2^-10 of the scale, which is at most a 224th of the maximum)
     top = np.repeat(np.pad(np.abs(z64) + off, (0, -N % 32)).reshape(-1, 32).max(1), 32)[:N]
     R.assert_within(got, z64 + np.zeros((M, 1)), off + np.maximum(2.0 ** -4 * (np.abs(z64) + off), 2.0 ** -10 * top / 224) + np.zeros((M, 1)), "z8")
+
+
+def test_slope_of_finite_arguments_is_finite():
+    """Squares of these are beyond binary32; the slope is 1 or 0 (squared ReLU: twice the argument)."""
+    far = [8.0, 50.0, 100.0, 101.0, 1e4, 1.8e19, 1.9e19, 1e20, 3e38]
+    z = torch.tensor([[s * v for v in far for s in (1, -1)] * 4], dtype=torch.bfloat16)
+    da = torch.full_like(z, 0.75)
+    for act in sorted(R.ACTS):
+        for kept in (z.cuda(), R.copy_on_gpu(R.f64(z))):
+            z64 = R.f64(z) if isinstance(kept, torch.Tensor) else R.decode8(*R.copy8(R.f64(z)))
+            dz, a, dbias = torch.empty_like(z).cuda(), torch.empty_like(z).cuda(), torch.empty(z.shape[1], device="cuda")
+            ws = torch.empty(B.nvfp4_act_bwd_workspace_bytes(*z.shape), dtype=torch.uint8, device="cuda")
+            B.nvfp4_act_bwd(da.cuda(), kept, R.ACTS[act], dz, a, dbias, workspace=ws)
+            with np.errstate(over="ignore", invalid="ignore"):
+                want, value = 0.75 * R.slope64(z64, act), R.act64(z64, act)
+            ok = np.abs(want) < 2.0 ** 127  # (twice the largest argument is beyond bf16)
+            # 256 u for the fast functions (see test_far_arguments_of_the_activations); results below 2^-126 may be zero
+            for got in (dz, dbias.view(1, -1)):
+                R.assert_within(R.f64(got)[ok], want[ok], ((BF16 + 256 * U) * np.abs(want) + 8 * U)[ok], act)
+            ok = np.abs(value) < 2.0 ** 127
+            R.assert_within(R.f64(a)[ok], value[ok], ((BF16 + 256 * U) * np.abs(value) + 2.0 ** -110)[ok], act)
