@@ -68,3 +68,43 @@ def test_slope_of_finite_arguments_is_finite():
                 R.assert_within(R.f64(got)[ok], want[ok], ((BF16 + 256 * U) * np.abs(want) + 8 * U)[ok], act)
             ok = np.abs(value) < 2.0 ** 127
             R.assert_within(R.f64(a)[ok], value[ok], ((BF16 + 256 * U) * np.abs(value) + 2.0 ** -110)[ok], act)
+
+
+@pytest.mark.parametrize("cols", [8, 40, 520, 1048, 2056, 5120, 10248, 20480, 30008])
+@pytest.mark.parametrize("res", [None, torch.bfloat16, torch.float32])
+def test_norm_of_rows_whose_squares_exceed_binary32(cols, res):
+    """Finite rows: mean and root are in 64 bits, so the norm is too."""
+    tops = [1.0, 3e17, 1.7e19, 1.9e19, 1e20, 1e30, 3e38]
+    rows = len(tops)
+    x = (torch.rand((rows, cols), generator=torch.Generator().manual_seed(cols)) * 2 - 1).double()
+    x[:, cols // 2] = 1.0  # (the largest)
+    x = x * torch.tensor(tops, dtype=torch.float64)[:, None]
+    gain = torch.rand(cols, generator=torch.Generator().manual_seed(cols + 1)) + 0.5
+    if res is None:
+        x, r = x.to(torch.bfloat16), None
+    else:
+        x, r = (x / 2).to(torch.bfloat16), (x / 2).to(res)
+    h = R.f64(x) if r is None else (R.f64(x) + R.f64(r)).astype(np.float32).astype(np.float64)
+    r64 = 1 / np.sqrt((h * h).mean(1) + 1e-5)
+    y64 = h * r64[:, None] * R.f64(gain)
+    y, rstd = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda"), torch.empty(rows, device="cuda")
+    y8 = B.alloc_tensor(rows, cols, format=B.FORMAT_MXFP8)
+    B.nvfp4_rmsnorm_fwd(x.cuda(), gain.cuda(), 1e-5, y, rstd, residual=r.cuda() if r is not None else None, y8=y8)
+    # (rstd of the last rows is below 2^-126: multiples of 2^-149)
+    R.assert_within(R.f64(rstd), r64, r64 * 2.0 ** -17 + 2.0 ** -150, "rstd")
+    off = 2.0 ** -17 + 4 * U + 2.0 ** -150 / r64[:, None]
+    R.assert_within(R.f64(y), y64, np.abs(y64) * (BF16 + off) + 1e-38, "y")
+    got = R.decode8(y8.codes.cpu().numpy(), y8.scales.cpu().numpy())
+    top = np.repeat(np.abs(np.pad(y64, ((0, 0), (0, -cols % 32))).reshape(rows, -1, 32)).max(2), 32, axis=1)[:, :cols]
+    R.assert_within(got, y64, np.maximum(2.0 ** -4 * np.abs(y64), 2.0 ** -10 * top / 224) * (1 + 2 * off) + off * np.abs(y64) + 1e-38, "y8")
+    # the gradient from the kept h and this rstd: nothing in it is beyond binary32 either
+    dy, kept = torch.rand((rows, cols), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16), x if r is None else torch.from_numpy(h).to(res)
+    dh, dgain = torch.empty((rows, cols), device="cuda"), torch.empty(cols, device="cuda")
+    ws = torch.empty(B.nvfp4_rmsnorm_bwd_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.nvfp4_rmsnorm_bwd(dy.cuda(), kept.cuda(), gain.cuda(), rstd, dh, dgain, ws)
+    k64, d64, s = R.f64(kept), R.f64(dy), R.f64(rstd)[:, None]
+    n, g = k64 * s, d64 * R.f64(gain)
+    c = (g * n).mean(1, keepdims=True)
+    tol = s * (8 * U * (np.abs(g) + np.abs(n * c)) + np.abs(n) * 2.0 ** -17 * np.abs(g * n).mean(1, keepdims=True))
+    R.assert_within(R.f64(dh), s * (g - n * c), tol + U * np.abs(s * (g - n * c)) + 1e-40, "dh")
+    R.assert_within(R.f64(dgain), (d64 * n).sum(0), (rows / 64 + 96) * U * np.abs(d64 * n).sum(0), "dgain")
