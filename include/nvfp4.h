@@ -59,7 +59,8 @@ enum { NVFP4_SF_LINEAR = 0, NVFP4_SF_SWIZZLED = 1 };
    vectors in its epilogue (D[i][j] = s_dec^A[i] * s_dec^B[j] * sum ...). */
 /* MXFP8 is the format of activations that are kept for the backward pass (no operand of nvfp4_gemm): E4M3 elements, one UE8M0
    power-of-two scale per 32 elements of a row, the smallest 2^E (E >= -127) with amax_b <= 448 * 2^E, no tensor-level scale.
-   Row-wise copies, rounding to nearest; nvfp4_quantize, nvfp4_rmsnorm_fwd and nvfp4_gemm_bf16_epilogue make them. */
+   Row-wise copies, rounding to nearest; nvfp4_quantize, nvfp4_rmsnorm_fwd and nvfp4_gemm_bf16_epilogue make them.  (Elements of
+   magnitude 248 * 2^120 and more round to the value 2^128, which binary32 and bf16 hold as infinity.) */
 enum { NVFP4_FORMAT_NVFP4 = 0, NVFP4_FORMAT_MXFP4 = 1, NVFP4_FORMAT_NVFP4_ROWSCALE = 2, NVFP4_FORMAT_MXFP8 = 3 };
 enum {
   /* the column-wise copy draws its stochastic-rounding bits from a second stream (bit 63 of
@@ -302,8 +303,9 @@ NVFP4_API nvfp4_status nvfp4_linear_fwd_noalloc(const void* X, const void* W, in
 /*
  * Around the linear layers: what makes their input, follows their product and is kept for their backward pass.
  * Matrices are row-major with a leading dimension in elements (>= cols); bf16 leading dimensions are multiples of 8, binary32 ones of
- * 4, pointers 16-byte aligned, cols a multiple of 8.  Any number of rows from one on.  Buffers overlap only where it is said that they may,
- * and calls that may run at the same time (two streams, two captured graphs) need workspaces of their own.
+ * 4, pointers 16-byte aligned, cols a multiple of 8.  Any number of rows from one on (nvfp4_linear_bf16_bwd8: multiples of 8).  Buffers
+ * overlap only where it is said that they may, and calls that may run at the same time (two streams, two captured graphs) need workspaces
+ * of their own.
  *
  * nvfp4_rmsnorm_fwd: h = x + residual (one binary32 addition; h = x without a residual), rstd = 1 / sqrt(mean(h^2) + eps) per row,
  *   y = h * rstd * gain.  y and the copies are taken of the binary32 h.
@@ -356,7 +358,9 @@ typedef struct nvfp4_epilogue {
  *   workspace: nvfp4_act_bwd_workspace_bytes(rows, cols), 256-byte aligned, for dbias (NULL without).
  * nvfp4_linear_bf16_bwd8: nvfp4_linear_bf16_bwd with X from its MXFP8 copy [M x K]: dW = dY^T X^, X^ the copy's values in bf16 (exact
  *   but below 2^-126).  dW adds up sums of 1024 products, rounded to nearest, where nvfp4_linear_bf16_bwd leaves the whole sum to the tensor
- *   cores, which cut it off at every addition.
+ *   cores, which cut it off at every addition.  M a multiple of 8, as in nvfp4_linear_bf16_bwd (NVFP4_ERR_SHAPE).  For other numbers of
+ *   tokens the caller keeps dY, the copy and dX in buffers with the rows up to the next multiple: with zeros in those of dY and finite
+ *   values in those of the copy they add nothing to dW, and dX has zeros there.
  *   workspace: nvfp4_linear_bf16_bwd8_workspace_bytes(M, K), 256-byte aligned, for X^ (NULL without dW).
  * nvfp4_dequantize_bf16: the values of an MXFP8 copy in bf16, leading dimension ld.
  */

@@ -108,3 +108,23 @@ def test_norm_of_rows_whose_squares_exceed_binary32(cols, res):
     tol = s * (8 * U * (np.abs(g) + np.abs(n * c)) + np.abs(n) * 2.0 ** -17 * np.abs(g * n).mean(1, keepdims=True))
     R.assert_within(R.f64(dh), s * (g - n * c), tol + U * np.abs(s * (g - n * c)) + 1e-40, "dh")
     R.assert_within(R.f64(dgain), (d64 * n).sum(0), (rows / 64 + 96) * U * np.abs(d64 * n).sum(0), "dgain")
+
+
+def test_layer_gradients_of_any_number_of_tokens():
+    """1003 tokens in buffers of 1008 rows: zeros behind them in dY, anything that is a number in the copy."""
+    M, rows, N, K = 1003, 1008, 264, 520
+    dy, w = (torch.randint(-2, 3, s, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16) for i, s in enumerate(((rows, N), (N, K))))
+    dy[M:] = 0
+    x = torch.randint(-4, 5, (rows, K), generator=torch.Generator().manual_seed(5)).to(torch.bfloat16)
+    x[M:] = 1000
+    x8 = B.alloc_tensor(rows, K, format=B.FORMAT_MXFP8)
+    B.nvfp4_quantize(x.cuda(), B.quant_opts(), x8)
+    dx, dw = torch.empty((rows, K), dtype=torch.bfloat16, device="cuda"), torch.empty((N, K), device="cuda")
+    ws = torch.empty(B.nvfp4_linear_bf16_bwd8_workspace_bytes(rows, K), dtype=torch.uint8, device="cuda")
+    B.nvfp4_linear_bf16_bwd8(dy.cuda(), x8, w.cuda(), dx, dw, ws)
+    assert np.array_equal(R.f64(dw), R.f64(dy[:M]).T @ R.f64(x[:M]))
+    assert np.array_equal(R.f64(dx[:M]), torch.from_numpy(R.f64(dy[:M]) @ R.f64(w)).to(torch.bfloat16).double().numpy())
+    assert not dx[M:].any()
+    with pytest.raises(RuntimeError, match="nvfp4_linear_bf16_bwd8"):
+        short = B.NVFP4Tensor(x8.codes, x8.scales, None, M, K, B.SF_LINEAR, B.FORMAT_MXFP8)
+        B.nvfp4_linear_bf16_bwd8(dy[:M].cuda(), short, w.cuda(), dx[:M], dw, ws)
