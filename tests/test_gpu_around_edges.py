@@ -1,5 +1,5 @@
 """Where the operators around the linear layers have little room: long contractions whose codes must not show how the tensor cores add,
-and finite arguments whose squares are beyond binary32."""
+finite arguments whose squares are beyond binary32, and roundings that are promised one by one."""
 import numpy as np
 import pytest
 import torch
@@ -128,3 +128,83 @@ def test_layer_gradients_of_any_number_of_tokens():
     with pytest.raises(RuntimeError, match="nvfp4_linear_bf16_bwd8"):
         short = B.NVFP4Tensor(x8.codes, x8.scales, None, M, K, B.SF_LINEAR, B.FORMAT_MXFP8)
         B.nvfp4_linear_bf16_bwd8(dy[:M].cuda(), short, w.cuda(), dx[:M], dw, ws)
+
+
+# ------------------------------------------------------------------------------------- roundings of the norm, one by one ----
+def whole_rows(rows, cols, seed):
+    """Whole numbers whose sums of squares binary32 holds exactly, whatever the order (below 2^24)."""
+    top = int((2.0 ** 24 / cols) ** 0.5 * 1.5) - 1  # (uniform in [-top, top]: a mean square of top^2 / 3)
+    h = torch.randint(-min(top, 255), min(top, 255) + 1, (rows, cols), generator=torch.Generator().manual_seed(seed))
+    h[h == 0] = 1
+    assert int((h.long() ** 2).sum(1).max()) < 2 ** 24
+    return h.to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("cols", [64, 1048, 5120, 20480, 41000])
+def test_reciprocal_root_is_rounded_once(cols):
+    """Where the sum of squares is exact, mean, root and reciprocal leave rstd at the binary32 number next to the true one: they are taken to
+    2^-45 and better, so that only a root within that of a border between two numbers could go the other way."""
+    h = whole_rows(512, cols, 7 + cols)
+    rstd = torch.empty(512, device="cuda")
+    B.nvfp4_rmsnorm_fwd(h.cuda(), None, 1e-5, rstd=rstd)
+    h64 = R.f64(h)
+    exact = 1 / np.sqrt((h64 * h64).mean(1) + float(np.float32(1e-5)))
+    assert np.array_equal(rstd.cpu().numpy(), exact.astype(np.float32))
+
+
+@pytest.mark.parametrize("cols", [1024, 5120, 20480, 40960])
+def test_y_of_a_copy_is_rounded_once_before_it_is_coded(cols):
+    """Gains that put y between 1.05 and 2.5 roundings of binary32 beside a border of two codes: with one rounding, by 2^-24 at most, each
+    must come out on its side of the border."""
+    rng = np.random.default_rng(cols)
+    h = whole_rows(1, cols, 3 + cols)
+    h64 = R.f64(h)[0]
+    rstd = 1 / np.sqrt((h64 * h64).mean() + float(np.float32(1e-5)))
+    borders = (R.GRID[8:118] + R.GRID[9:119]) / 2  # (of normal codes up to 240)
+    want = rng.choice(borders, cols) * np.sign(h64)
+    want[::32] = 300.0 * np.sign(h64[::32])  # (every block's maximum: a scale of one)
+    gain = (want / (h64 * rstd) * (1 + rng.uniform(-4, 4, cols) * U)).astype(np.float32)
+    y64 = h64 * rstd * gain.astype(np.float64)
+    beside = np.abs(y64 / want - 1) / U
+    tested = (beside > 1.05) & (beside < 2.5)
+    tested[::32] = False
+    assert tested.sum() > cols // 4
+    y8 = B.alloc_tensor(1, cols, format=B.FORMAT_MXFP8)
+    B.nvfp4_rmsnorm_fwd(h.cuda(), torch.from_numpy(gain).cuda(), 1e-5, y8=y8)
+    codes, scales = R.copy8(y64[None])
+    assert np.array_equal(y8.scales.cpu().numpy(), scales)
+    got = y8.codes.cpu().numpy()[0]
+    assert np.array_equal(got[tested], codes[0][tested]), int((got[tested] != codes[0][tested]).sum())
+
+
+# ------------------------------------------------------------------------------------- layer gradients, in their bounds ----
+@pytest.mark.parametrize("shape", [(8, 24, 40), (1000, 264, 136), (200, 520, 1048), (2056, 1032, 520)])
+def test_layer_gradients_from_a_copy_stay_in_their_buffers(shape):
+    """Whole numbers, so that both gradients are known to the bit; what lies around every buffer stays as it was."""
+    M, N, K = shape
+    dy, w = (torch.randint(-2, 3, s, generator=torch.Generator().manual_seed(i)).to(torch.bfloat16) for i, s in enumerate(((M, N), (N, K))))
+    x = torch.randint(-4, 5, (M, K), generator=torch.Generator().manual_seed(5)).double().numpy()
+    dyd, dy_ok = R.guarded(M, N, torch.bfloat16, fill=dy.cuda())
+    wd, w_ok = R.guarded(N, K, torch.bfloat16, fill=w.cuda())
+    x8, x_ok = R.guarded_copy(M, K)
+    codes, scales = R.copy8(x)
+    x8.codes.copy_(torch.from_numpy(codes))
+    x8.scales.copy_(torch.from_numpy(scales))
+    dx, dx_ok = R.guarded(M, K, torch.bfloat16)
+    dw, dw_ok = R.guarded(N, K, torch.float32, fill=torch.full((N, K), 3.0, device="cuda"))
+    need = B.nvfp4_linear_bf16_bwd8_workspace_bytes(M, K)
+    held = torch.full((need + 512,), 77, dtype=torch.uint8, device="cuda")
+    at = -held.data_ptr() % 256
+    for tile in (0, 512, 640, 642, 644):
+        dw.fill_(3.0)
+        dx.fill_(float("nan"))
+        B.nvfp4_set_gemm_tile_n(tile)
+        try:
+            B.nvfp4_linear_bf16_bwd8(dyd, x8, wd, dx, dw, held[at:at + need], accumulate_dw=True)
+            B.nvfp4_device_status()
+        finally:
+            B.nvfp4_set_gemm_tile_n(0)
+        assert np.array_equal(R.f64(dw), R.f64(dy).T @ x + 3.0), tile
+        assert np.array_equal(R.f64(dx), torch.from_numpy(R.f64(dy) @ R.f64(w)).to(torch.bfloat16).double().numpy()), tile
+        assert all(ok() for ok in (dy_ok, w_ok, x_ok, dx_ok, dw_ok)), tile
+        assert bool((held[:at] == 77).all()) and bool((held[at + need:] == 77).all()), tile
