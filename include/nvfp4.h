@@ -348,7 +348,7 @@ typedef struct nvfp4_epilogue {
 } nvfp4_epilogue;
 /*
  * nvfp4_gemm_bf16_epilogue: the product of nvfp4_gemm_bf16 for K-major operands (X [M x K], W [N x K]) with the above in its epilogue,
- *   in binary32 until D (bf16) is rounded (with z8, sums of 1024 products are added up rounded to nearest, as in nvfp4_linear_bf16_bwd8).
+ *   in binary32 until D (bf16) is rounded (with z8, sums of at most 1024 products are added up rounded to nearest, of fewer where K is short).
  *   M any number from one on; N, K multiples of 8; lda, ldb, ldd, ldr, ldz multiples of 8; pointers
  *   16-byte aligned.
  * nvfp4_act_bwd: dz = da * act'(z) (bf16), a = act(z) (bf16: the next layer's input made again for its weight gradient),

@@ -744,10 +744,10 @@ static bool make_bf16_maps(const DenseGemmArgs& g, CUtensorMap* m) {  // A, B, D
 
 static int bf16_tiles(const DenseGemmArgs& g, int bn) { return ((g.M + 255) / 256) * ((g.N + bn - 1) / bn); }
 
-template <int BN, int SPLIT, bool TWO, class E = dense::NoEpilogue, int SHARE = 0>
+template <int BN, int SPLIT, bool TWO, class E = dense::NoEpilogue, bool SHARES = false>
 static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemmArgs* g1, const Bf16Wide& wide_cols, int max_pairs,
-                                        cudaStream_t s, const E& epilogue = E{}) {
-  auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO, E, SHARE>;
+                                        cudaStream_t s, const E& epilogue = E{}, int share = 0) {
+  auto kern = dense::gemm_bf16_pair_kernel<BN, SPLIT, TWO, E, SHARES>;
   constexpr int smem = dense::Cfg<BN, SPLIT>::kSmemBytes + E::kSmemBytes - (E::kBuffers ? dense::Cfg<BN, SPLIT>::kStageBytes : 0);
   static_assert(smem <= 232448, "shared memory budget");
   CUtensorMap m[6];
@@ -784,6 +784,7 @@ static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemm
     a.n_tiles0 = bf16_tiles(g0, BN);
     a.n_tiles = a.n_tiles0 + (g1 ? bf16_tiles(*g1, BN) : 0);
   }
+  a.share = share;
   const int pairs = a.n_tiles < max_pairs || SPLIT > 1 ? a.n_tiles : max_pairs;  // SPLIT > 1: a cluster for each tile
   const cudaError_t e = launch_kernel(kern, dim3(2 * SPLIT * pairs), dim3(dense::kThreads), smem, s, m[0], m[1], m[2],
                                       m[3], m[4], m[5], a, epilogue);
@@ -791,9 +792,9 @@ static cudaError_t launch_bf16_problems(const DenseGemmArgs& g0, const DenseGemm
   return e;
 }
 
-template <int BN, int SPLIT = 1, class E = dense::Epilogue, int SHARE = 0>
+template <int BN, int SPLIT = 1, class E = dense::Epilogue, bool SHARES = false>
 static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& a, const Bf16Wide& wide_cols, int max_pairs,
-                                        cudaStream_t s) {
+                                        cudaStream_t s, int share = 0) {
   E e{};
   auto map_of = [&](CUtensorMap* map, const void* p, int64_t ld) {
     return make_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, (uint64_t)g.N, (uint64_t)g.M, (uint64_t)ld * 2, SPLIT == 4 ? 32 : 64,
@@ -807,15 +808,15 @@ static cudaError_t launch_bf16_epilogue(const DenseGemmArgs& g, const EpilogueAr
   e.act = a.act;
   e.has_residual = a.residual != nullptr;
   e.has_z = a.z != nullptr;
-  return launch_bf16_problems<BN, SPLIT, false, E, SHARE>(g, nullptr, wide_cols, max_pairs, s, e);
+  return launch_bf16_problems<BN, SPLIT, false, E, SHARES>(g, nullptr, wide_cols, max_pairs, s, e, share);
 }
 
 // g1 == nullptr: one problem
-template <int BN, int SPLIT = 1, int SHARE = 0>
+template <int BN, int SPLIT = 1, bool SHARES = false>
 static cudaError_t launch_bf16_t(const DenseGemmArgs& g0, const DenseGemmArgs* g1, const Bf16Wide& wide_cols, int max_pairs,
-                                 cudaStream_t s) {
-  return g1 ? launch_bf16_problems<BN, SPLIT, true, dense::NoEpilogue, SHARE>(g0, g1, wide_cols, max_pairs, s)
-            : launch_bf16_problems<BN, SPLIT, false, dense::NoEpilogue, SHARE>(g0, nullptr, wide_cols, max_pairs, s);
+                                 cudaStream_t s, int share = 0) {
+  return g1 ? launch_bf16_problems<BN, SPLIT, true, dense::NoEpilogue, SHARES>(g0, g1, wide_cols, max_pairs, s, {}, share)
+            : launch_bf16_problems<BN, SPLIT, false, dense::NoEpilogue, SHARES>(g0, nullptr, wide_cols, max_pairs, s, {}, share);
 }
 
 static Bf16Wide bf16_wide_tiles(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int pairs) {
@@ -875,10 +876,10 @@ cudaError_t launch_gemm_bf16_shares(const DenseGemmArgs& g0, const DenseGemmArgs
   if (e != cudaSuccess) return e;
   const int pairs = num_sms / 2;
   const Bf16Wide none{{0, 0}};
-  if (tile == kTileSplit4) return launch_bf16_t<128, 4, dense::kShare>(g0, g1, none, pairs, s);
-  if (tile == kTileSplit2) return launch_bf16_t<128, 2, dense::kShare>(g0, g1, none, pairs, s);
-  if (tile == kTilePair128) return launch_bf16_t<128, 1, dense::kShare>(g0, g1, none, pairs, s);
-  return launch_bf16_t<256, 1, dense::kShare>(g0, g1, none, pairs, s);
+  if (tile == kTileSplit4) return launch_bf16_t<128, 4, true>(g0, g1, none, pairs, s, dense::kShare);
+  if (tile == kTileSplit2) return launch_bf16_t<128, 2, true>(g0, g1, none, pairs, s, dense::kShare);
+  if (tile == kTilePair128) return launch_bf16_t<128, 1, true>(g0, g1, none, pairs, s, dense::kShare);
+  return launch_bf16_t<256, 1, true>(g0, g1, none, pairs, s, dense::kShare);
 }
 
 cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs& e, int tile, const Bf16Wide& wide, cudaStream_t s) {
@@ -887,10 +888,12 @@ cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs
   if (err != cudaSuccess) return err;
   const int pairs = num_sms / 2;
   if (e.z8_codes) {
-    if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4, dense::Epilogue, dense::kShare>(g, e, wide, pairs, s);
-    if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2, dense::Epilogue, dense::kShare>(g, e, wide, pairs, s);
-    if (tile == kTilePair128) return launch_bf16_epilogue<128, 1, dense::Epilogue, dense::kShare>(g, e, wide, pairs, s);
-    return launch_bf16_epilogue<256, 1, dense::Epilogue, dense::kShare>(g, e, Bf16Wide{{0, 0}}, pairs, s);
+    const int pairs_of_tile = tile == kTileSplit4 ? 4 : tile == kTileSplit2 ? 2 : 1, blocks = (g.K + 63) / 64;
+    const int share = even_share((blocks + pairs_of_tile - 1) / pairs_of_tile, code_share(g.K));
+    if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4, dense::Epilogue, true>(g, e, wide, pairs, s, share);
+    if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2, dense::Epilogue, true>(g, e, wide, pairs, s, share);
+    if (tile == kTilePair128) return launch_bf16_epilogue<128, 1, dense::Epilogue, true>(g, e, wide, pairs, s, share);
+    return launch_bf16_epilogue<256, 1, dense::Epilogue, true>(g, e, Bf16Wide{{0, 0}}, pairs, s, share);
   }
   if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4>(g, e, wide, pairs, s);
   if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2>(g, e, wide, pairs, s);

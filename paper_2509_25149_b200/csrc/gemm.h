@@ -76,6 +76,20 @@ struct DenseGemmArgs {
 // The tile of such a launch: kTilePair256, kTilePair128, kTileDouble (*wide: how many column tiles of each product are 512 wide) or a
 // split one (`forced`, where every share has a k-block, or by size)
 int bf16_tile(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int forced, Bf16Wide* wide);
+// Products that keep z in 8 bits: the most k-blocks of 64 that a tensor-core accumulator takes before what it holds is added, rounded to nearest, to sums
+// outside.  An addition cuts off what the accumulator cannot hold, and the codes decide: with shares of this many they come out a step off at
+// most about twice as often as with binary32 sums (error of the copy's values below 1.5 times theirs).  Of 2 * 2048 x 4096 codes, binary32 / shares of 4,
+// 6, 8, 12, 16 blocks: K of 512 102 / 170, 198, 300 (one share); 1024 153 / 161, 226, 320, 432, 639; 2048 218 / 176, 244, 357, 478, 684; 4096 360 /
+// 157, 243, 297, 483, 680; 20480 999 / 192, 268, 332, 486, 668.  Short shares wait for the warps that read the accumulators (SHARES in gemm_bf16.cuh).
+inline int code_share(int K) {
+  const int blocks = (K + 63) / 64;
+  return blocks <= 5 ? 5 : blocks <= 8 ? 4 : blocks <= 24 ? 8 : blocks <= 100 ? 12 : 16;
+}
+// `blocks` in as many parts as that takes, of a size: that size (the last may have fewer)
+inline int even_share(int blocks, int most) {
+  const int parts = (blocks + most - 1) / most;
+  return (blocks + parts - 1) / parts;
+}
 // The same with sums of 1024 products at most added up outside the tensor cores (SHARE in gemm_bf16.cuh); no 512-wide tiles
 cudaError_t launch_gemm_bf16_shares(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, cudaStream_t s);
 // What follows a product (nvfp4_gemm_bf16_epilogue): z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits

@@ -53,6 +53,7 @@ struct Args {
   // BN = 512: tiles 512 columns wide of problem 0 and 1, then the tiles 256 wide of both, and where each of these four ends
   int wide_n[2];  // column tiles 512 wide of each problem
   int seg_end[4];
+  int share;  // SHARES: k-blocks that an accumulator takes at most
 };
 
 // What follows a product: z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits (a launch with one problem)
@@ -255,23 +256,24 @@ __device__ __forceinline__ void tc2_mma_bf16(uint32_t d_tmem, uint64_t adesc, ui
 // each pair a share of the k-blocks (the exchange: pair::exchange_columns).
 // TWO: the launch has two problems.
 // E: Epilogue (EpilogueBuffers) or NoEpilogue.
-// SHARE > 0: an accumulator takes no more than SHARE k-blocks.  Then the issuer goes on in the other one, and the epilogue warps add what it
+// SHARES: an accumulator takes no more than Args::share k-blocks.  Then the issuer goes on in the other one, and the epilogue warps add what it
 // holds to sums of their own, rounded to nearest.  The tensor cores cut off what an addition to an accumulator cannot hold, an error that
 // grows with every one of them: a weight gradient over 16384 tokens (values of an 8-bit copy) is 8.6e-6 off in the mean square, 3.1e-5 where all
-// terms have one sign; in shares of 8 / 16 k-blocks 1.9e-7 / 2.3e-7 and 3.9e-7 / 6.3e-7.  What it costs is the power of reading the
-// accumulators more often (8192 x 20480 x 5120 with codes of 8 bits, at the power limit: 1370 us in one sum, 1419 in shares of 16, 1505 of
-// 8) and, where a share is as short as the epilogue of the tile before, waiting for that.  Of such codes 1.7 times as many come out a step off
-// as with sums in binary32 in shares of 16, as many in shares of 8, three times as many in shares of 32.
+// terms have one sign; in shares of 8 / 16 k-blocks 1.9e-7 / 2.3e-7 and 3.9e-7 / 6.3e-7.  Weight gradients take shares of kShare, 1024 products;
+// codes of 8 bits want shorter ones where the contraction is short (code_share in gemm.h).  What it costs is waiting for the epilogue of the tile
+// before, and the power of reading the accumulators more often: 8192 x 20480 x 5120 with codes of 8 bits, in a loop at the power limit, 1326 us in one
+// sum, in shares of 8 / 12 / 16 1365 / 1302 / 1288 (on another GPU 1410 / 1360 / 1340); x 2048 591 / 560 / 552; x 1024 333 / 328 / 315 (one share); x 512
+// 237 in one share, 252 in shares of 4.
 // Not for 512-wide tiles, whose halves need both accumulators.
 constexpr int kShare = 16;
-template <int BN, int SPLIT = 1, bool TWO = true, class E = NoEpilogue, int SHARE = 0>
+template <int BN, int SPLIT = 1, bool TWO = true, class E = NoEpilogue, bool SHARES = false>
 __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_bf16_pair_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_b0,
                           const __grid_constant__ CUtensorMap map_d0, const __grid_constant__ CUtensorMap map_a1,
                           const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_d1,
                           const __grid_constant__ Args g, const __grid_constant__ E e) {
   static_assert(!E::kFused || !TWO, "an epilogue belongs to one product");
-  static_assert(SHARE == 0 || BN < 512, "two accumulators in turn");
+  static_assert(!SHARES || BN < 512, "two accumulators in turn");
   using namespace pair;
   static_assert(!E::kBuffers || (BN == 256 && SPLIT == 1), "two chunks to a group");
   constexpr int S = dense::Cfg<BN, SPLIT>::kStages - (E::kBuffers ? 1 : 0), kStageBytes = dense::Cfg<BN, SPLIT>::kStageBytes;
@@ -500,8 +502,12 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
               return;
             }
           }
+          int left = SHARES ? g.share : 0;  // k-blocks of this share
+          bool first = true;
           for (int kb = 0; kb < k_blocks; ++kb) {
-            if (SHARE > 0 && kb > 0 && kb % (SHARE > 0 ? SHARE : 1) == 0) {  // this share is complete; on in the other accumulator
+            if (SHARES && left-- == 0) {  // this share is complete; on in the other accumulator
+              left = g.share - 1;
+              first = true;
               tc2_commit_both(accf_bar(buf), pair_mask);
               acc_phase ^= 1u << buf;
               buf ^= 1;
@@ -509,7 +515,8 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
               tc_fence_after();
             }
             if (!landed(stage, phase)) return;
-            mma(stage, 0, buf, SHARE > 0 ? kb % (SHARE > 0 ? SHARE : 1) == 0 : kb == 0);
+            mma(stage, 0, buf, SHARES ? first : kb == 0);
+            first = false;
             release();
           }
         };
@@ -574,8 +581,8 @@ __global__ void __cluster_dims__(2 * SPLIT, 1, 1) __launch_bounds__(kThreads, 1)
       }
       const int row0 = m_blk * 256 + (int)rank * 128;
       uint32_t r[HN / 2];
-      if constexpr (SHARE > 0) {
-        const int shares = (k_begin(tile, split + 1) - k_begin(tile, split) + SHARE - 1) / SHARE;
+      if constexpr (SHARES) {
+        const int shares = (k_begin(tile, split + 1) - k_begin(tile, split) + g.share - 1) / g.share;
         bool gave_up = false;
 #pragma unroll
         for (int j = 0; j < HN / 2; ++j) r[j] = 0u;

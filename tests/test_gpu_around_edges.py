@@ -208,3 +208,39 @@ def test_layer_gradients_from_a_copy_stay_in_their_buffers(shape):
         assert np.array_equal(R.f64(dx), torch.from_numpy(R.f64(dy) @ R.f64(w)).to(torch.bfloat16).double().numpy()), tile
         assert all(ok() for ok in (dy_ok, w_ok, x_ok, dx_ok, dw_ok)), tile
         assert bool((held[:at] == 77).all()) and bool((held[at + need:] == 77).all()), tile
+
+
+def steps_off(M, N, K, seed):
+    """Codes of z = A B^T + bias that are not those of z in 64 bits: of the call's and of a copy of the product in binary32."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    a, b = (torch.randn(s, generator=g, device="cuda").to(torch.bfloat16) for s in ((M, K), (N, K)))
+    bias = torch.randn(N, generator=g, device="cuda") * K ** 0.5
+    z, D = B.alloc_tensor(M, N, format=B.FORMAT_MXFP8), torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    B.nvfp4_gemm_bf16_epilogue(a, b, D, bias, z=z)
+    B.nvfp4_device_status()
+    exact = torch.cat([torch.addmm(bias.double(), p.double(), b.double().t()) for p in a.split(256)])
+    blocks = exact.view(M, N // 32, 32)
+    m, e = torch.frexp(blocks.abs().amax(2, keepdim=True))
+    scale = torch.ldexp(torch.ones_like(m), torch.where(m <= 0.875, e - 9, e - 8))  # (448 = 0.875 * 2^9)
+    v = blocks / scale
+    step = torch.ldexp(torch.ones_like(v), torch.frexp(v.abs().clamp_min(2.0 ** -6))[1] - 4)
+    want = (torch.round(v / step) * step * scale).view(M, N)
+    plain = B.alloc_tensor(M, N, format=B.FORMAT_MXFP8)
+    torch.backends.cuda.matmul.allow_tf32 = False
+    B.nvfp4_quantize(a.float() @ b.float().t() + bias, B.quant_opts(), plain)
+    return (int((B.nvfp4_dequantize(q).double() != want).sum()) for q in (z, plain))
+
+
+# rows, columns, contraction, draws: one, two, three and more shares of every length, each kernel
+OFF = [(2048, 4096, K, 1) for K in (520, 776, 1024, 1096, 1536, 1608, 2048, 4096, 5120, 8200)]
+
+
+@pytest.mark.parametrize("M,N,K,draws", OFF)
+def test_codes_are_about_as_exact_as_those_of_binary32_sums(M, N, K, draws):
+    """A code is a step off where the error of z carries it across a border, so their number goes with the error, and their error in the mean
+    square with its root: 1.5 times that of binary32 sums is 2.25 times as many.  (Counts have deviations of their root: four of both.)"""
+    mine = plain = 0
+    for seed in range(draws):
+        x, y = steps_off(M, N, K, 200 + seed)
+        mine, plain = mine + x, plain + y
+    assert mine <= 2.25 * plain + 4 * (mine + 2.25 ** 2 * plain) ** 0.5, (mine, plain)
