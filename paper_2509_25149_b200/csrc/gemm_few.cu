@@ -30,11 +30,14 @@ struct Ring {
   static_assert(kPart + kTotal <= kBytes, "the sums reuse the ring");
 };
 
-// SHARES: an accumulator takes no more than kShareSteps steps, 1024 products, and is then added to sums in registers, rounded to nearest: what
-// the instructions cut off grows with the length of a chain, and codes of 8 bits show it (65536 products of one sign in four chains, each a
-// warp's: 7.6e-5 of the sum off, in shares 8.7e-7).  For calls that keep z in 8 bits and whose chains would be longer: one row x 5120 x 20480
-// 41.9 / 42.7 us, 16 rows 49.5 / 50.3, 32 x 16384 x 16384 120 / 127 (the whole sum / in shares; the registers of the second set of sums).
-constexpr int kShareSteps = 32;
+// SHARES: an accumulator takes no more than kShareSteps steps, 128 or 256 products, and is then added to sums in registers, rounded to nearest:
+// what the instructions cut off grows with the length of a chain, and codes of 8 bits show it.  For calls that keep z in 8 bits.  65536 products of one
+// sign in four chains, each a warp's, are 7.6e-5 of the sum off, in shares of 1024 8.7e-7.  Of random ones with 8 x 20480 x 4096 (12 draws) codes
+// come out a step off: with the products in binary32 14, with whole chains 87, in shares of 256 / 128 products 27 / 17; 32 x 8192 x 5120 73, 165,
+// 31 / 19.  One row x 5120 x 5120 takes 11.4 / 11.8 us (whole chains / these shares), x 20480 42.3 / 43.6, 16 rows 49.4 / 50.7, 32 x 16384 x 16384 120 / 128
+// (the registers of the second set of sums).
+template <int MT>
+constexpr int kShareSteps = MT < 4 ? 4 : 8;
 template <int MT, int ST, bool SHARES>
 __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) {
   using R = Ring<MT, ST>;
@@ -81,10 +84,10 @@ __global__ void __launch_bounds__(32 * kWarps) few_rows_kernel(const FewArgs g) 
 #pragma unroll
   for (int u = 0; u < ST - 1; ++u) fetch(s0 + u, u);
   float acc[2][MT][4] = {}, sums[SHARES ? 2 : 1][SHARES ? MT : 1][4] = {};
-  int slot = 0, next = ST - 1, until = s0 + kShareSteps;
+  int slot = 0, next = ST - 1, until = s0 + kShareSteps<MT>;
   for (int s = s0; s < s1; ++s) {
     if (SHARES && s == until) {
-      until += kShareSteps;
+      until += kShareSteps<MT>;
 #pragma unroll
       for (int i = 0; i < 8 * MT; ++i) {
         float& a = acc[i / (4 * MT)][i / 4 % MT][i % 4];
@@ -164,7 +167,7 @@ cudaError_t launch_few(const FewArgs& a, cudaStream_t s) {
 template <int MT, int ST>
 cudaError_t launch_few(const FewArgs& a, cudaStream_t s) {
   const int steps = (a.K + 31) / 32, warps = kWarps * a.shares;
-  return a.z8.codes && steps > kShareSteps * warps ? launch_few<MT, ST, true>(a, s) : launch_few<MT, ST, false>(a, s);
+  return a.z8.codes && steps > kShareSteps<MT> * warps ? launch_few<MT, ST, true>(a, s) : launch_few<MT, ST, false>(a, s);
 }
 }  // namespace
 
