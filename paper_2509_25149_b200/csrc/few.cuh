@@ -18,6 +18,7 @@ struct FewArgs {
   Copy8 z8;
   int64_t lda, ldb, ldd, ldr, ldz;
   int M, N, K, act, shares;  // shares: CTAs of a cluster
+  int chain;                 // tokens_kernel with z in 8 bits: k-blocks of an accumulator
 };
 
 inline FewArgs few_args(const DenseGemmArgs& g, const EpilogueArgs& e) {

@@ -905,7 +905,7 @@ cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs
   return e.residual && g.K <= 1024 ? launch_bf16_epilogue<256, 1, dense::EpilogueBuffers>(g, e, wide, pairs, s) : launch_bf16_epilogue<256>(g, e, wide, pairs, s);
 }
 
-template <int MT, int ST>
+template <int MT, int ST, bool ACCS>
 static cudaError_t launch_tokens(const DenseGemmArgs& g, const FewArgs& a, cudaStream_t s) {
   using C = tokens::Cfg<MT, ST>;
   CUtensorMap map_w, map_x;
@@ -913,7 +913,7 @@ static cudaError_t launch_tokens(const DenseGemmArgs& g, const FewArgs& a, cudaS
   if (!make_map_2d(&map_w, bf, 2, g.b, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldb * 2, 64, tokens::kCols, true) ||
       !make_map_2d(&map_x, bf, 2, g.a, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda * 2, 64, MT, true))
     return cudaErrorInvalidValue;
-  auto kern = tokens::tokens_kernel<MT, ST>;
+  auto kern = tokens::tokens_kernel<MT, ST, ACCS>;
   static std::atomic<uint64_t> configured{0};  // per instantiation and device
   int dev;
   if (device_needs_config(configured, &dev)) {
@@ -937,6 +937,9 @@ static int token_shares(int64_t N, int64_t K, int sms) {
   return s < 1 ? 1 : (int)s;
 }
 
+static int token_columns(int M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }  // of an accumulator
+static int token_blocks(int K, int shares) { return ((K + 63) / 64 + shares - 1) / shares; }  // k-blocks of a CTA, at most
+
 // Where that is faster than the few-rows kernel (up to 32 rows of A) and the pair kernels; here / there, us, weights that exceed L2 together:
 //   up to 8 rows   large weights: 20480 x 5120 35.9 / 38.4, 5120 x 20480 35.4 / 40.1, but 7168 x 5120 15.5 / 14.5, 4096 x 4096 9.9 / 8.4
 //   up to 16       5120 x 5120 12.4 / 13.7, 7168 x 5120 15.4 / 16.1, but 8192 x 2048 9.7 / 8.2, 1024 x 16384 12.9 / 11.2
@@ -946,12 +949,13 @@ static int token_shares(int64_t N, int64_t K, int sms) {
 //   up to 128      (128 rows) 5120 x 5120 17.6 / 25.7, 5120 x 20480 42.8 / 89, 20480 x 5120 47.5 / 60.4, but 2048 x 2048 9.8 / 9.1, 8192 x 2048
 //                  14.8 / 13.2, and where 256-wide tiles are nearly a round of the pairs: 14336 x 4096 31.5 / 28.6, 16384 x 4096 33.7 / 29.6
 // (256 rows are as many bytes from L2 as two tiles of B: 5120 x 5120 26.0 / 26.1, 20480 x 5120 87 / 62.)
-// Codes of 8 bits want sums of no more than kShare k-blocks.
+// Codes of 8 bits want sums of no more than code_share k-blocks; up to 16 rows, whose products in binary32 torch takes in many parts, of four.
 bool gemm_tokens_pays(const DenseGemmArgs& g, const EpilogueArgs& e) {
   int sms = 0;
   if (g.M > kTokenRows || sm_count(&sms) != cudaSuccess) return false;
-  const int64_t blocks = ((int64_t)g.K + 63) / 64, weight = (int64_t)g.N * g.K;
-  if (e.z8_codes && blocks > (int64_t)dense::kShare * token_shares(g.N, g.K, sms)) return false;
+  const int64_t weight = (int64_t)g.N * g.K;
+  const int most = (g.M <= 16 ? 4 : code_share(g.K)) * (256 / token_columns(g.M));
+  if (e.z8_codes && token_blocks(g.K, token_shares(g.N, g.K, sms)) > most) return false;
   if (g.M <= 16) return weight >= (g.M <= 8 ? 40000000 : 20000000) && g.N > 15 * tokens::kCols;
   if (g.M <= 32) return weight >= 5000000 && g.N > 7 * tokens::kCols;
   if (g.M <= 64) return g.K >= 1024 || g.N > (int64_t)sms * tokens::kCols;
@@ -965,7 +969,13 @@ cudaError_t launch_gemm_tokens(const DenseGemmArgs& g, const EpilogueArgs& e, cu
   const cudaError_t err = sm_count(&sms);
   if (err != cudaSuccess) return err;
   a.shares = token_shares(g.N, g.K, sms);
-  return g.M <= 32 ? launch_tokens<32, 5>(g, a, s) : g.M <= 64 ? launch_tokens<64, 4>(g, a, s) : launch_tokens<128, 3>(g, a, s);
+  const int blocks = token_blocks(g.K, a.shares), columns = token_columns(g.M);
+  if (e.z8_codes && blocks > 1) {
+    // (shorter chains than that gain nothing, and every accumulator costs a reading: 32 x 5120 x 5120 14.7 us with chains of two, 14.5 of four)
+    a.chain = std::max(g.M <= 16 ? 2 : 4, (blocks + 256 / columns - 1) / (256 / columns));
+    return columns == 32 ? launch_tokens<32, 5, true>(g, a, s) : columns == 64 ? launch_tokens<64, 4, true>(g, a, s) : launch_tokens<128, 3, true>(g, a, s);
+  }
+  return columns == 32 ? launch_tokens<32, 5, false>(g, a, s) : columns == 64 ? launch_tokens<64, 4, false>(g, a, s) : launch_tokens<128, 3, false>(g, a, s);
 }
 
 // Test aid: one warp waits, with the given limit, on a barrier nobody arrives at.  The wait runs out, the code lands

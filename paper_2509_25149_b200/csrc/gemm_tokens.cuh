@@ -48,7 +48,15 @@ __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t adesc, uint64
       : "memory");
 }
 
-template <int MT, int ST>
+// Accumulators of a CTA, all that two to an SM leave room for.
+template <int MT>
+constexpr int kAccs = 256 / MT;
+
+// ACCS: a CTA's k-blocks go to several accumulators, g.chain blocks to each, and what these hold is added rounded to nearest (for codes of 8 bits, see
+// code_share in gemm.h): nothing waits, since each is written in one run and read at the end.  16 x 8192 x 4096 (16 draws): 11 codes a step off for 18 of
+// products in binary32 (with one accumulator 85), 64 x 5120 x 20480 87 for 159.  64 x 5120 x 5120 16.8 / 16.9 us (one / several), 16 rows 13.1 / 13.6; longer
+// contractions, which one accumulator was too short for, 64 x 5120 x 20480 95 (pair kernel) / 41.8, 32 rows 59.6 (gemm_few.cu) / 38.4.
+template <int MT, int ST, bool ACCS>
 __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                                                           const __grid_constant__ FewArgs g) {
   using C = Cfg<MT, ST>;
@@ -65,6 +73,7 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
   const int rank = g.shares > 1 ? (int)cluster_rank() : 0;
   const int n0 = (int)(blockIdx.x / (unsigned)g.shares) * kCols;
   const int blocks = (g.K + 63) / 64, tiles = (g.N + kCols - 1) / kCols;
+  const uint32_t columns = MT * (ACCS ? kAccs<MT> : 1);
   const int k0 = (int)((int64_t)blocks * rank / g.shares), k1 = (int)((int64_t)blocks * (rank + 1) / g.shares);  // (never empty: see the launch)
 
   if (threadIdx.x == 0) {
@@ -82,7 +91,7 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(MT) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(columns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -116,14 +125,23 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
     bool ok = true;
     const uint32_t w_lo0 = ((base >> 4) & 0x3fffu) | (1u << 16), x_lo0 = (((base + kCols * 128) >> 4) & 0x3fffu) | (1u << 16);
     constexpr uint32_t idesc = dense::instr_desc_bf16(kCols, MT, 0, 0);
+    uint32_t d = tmem;
+    int left = ACCS ? g.chain : 0;
+    bool first = true;
     for (int kb = k0; kb < k1; ++kb) {
+      if (ACCS && left-- == 0) {
+        left = g.chain - 1;
+        first = true;
+        d += MT;
+      }
       if (!(ok = mbar_wait(full_bar(stage), phase, abort_flag, 0xF20u + stage))) break;
       tc_fence_after();
       const uint32_t at = stage * (C::kStage >> 4);
 #pragma unroll
       for (int j = 0; j < 4; ++j)  // 16 k: 32 bytes further inside the 128-byte swizzle span
-        mma_bf16(tmem, make_desc(w_lo0 + at + 2 * j, kDescHiOperand), make_desc(x_lo0 + at + 2 * j, kDescHiOperand), idesc,
-                 kb > k0 || j > 0 ? 1u : 0u);
+        mma_bf16(d, make_desc(w_lo0 + at + 2 * j, kDescHiOperand), make_desc(x_lo0 + at + 2 * j, kDescHiOperand), idesc,
+                 !first || j > 0 ? 1u : 0u);
+      first = false;
       tc_commit(empty_bar(stage));
       if (++stage == ST) {
         stage = 0;
@@ -142,6 +160,7 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
   ok = __all_sync(0xffffffffu, ok);
   tc_fence_after();
   const uint32_t row = tmem + ((uint32_t)(32 * warp) << 16);
+  const int accs = ACCS ? (k1 - k0 + g.chain - 1) / g.chain : 1;
   if (g.shares > 1) {
     // Row m goes to rank m mod shares, as its row m / shares of this share: [share][row][row of B]
     const int own = (g.M + g.shares - 1) / g.shares;
@@ -155,6 +174,15 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
         uint32_t r[32];
         tc_ld32(row + c, r);
         tc_wait_ld();
+        if (ACCS)
+#pragma unroll 1
+          for (int a = 1; a < accs; ++a) {
+            uint32_t more[32];
+            tc_ld32(row + a * MT + c, more);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) + __uint_as_float(more[j]));
+          }
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           if (c + j < g.M) st_of_rank(at, (uint32_t)owner, r[j]);
@@ -190,6 +218,14 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
       float v[kOwn];
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) v[j] = __uint_as_float(r[j]);
+      if (ACCS)
+#pragma unroll 1
+        for (int a = 1; a < accs; ++a) {
+          tc_ld8(row + a * MT + c, r);
+          tc_wait_ld();
+#pragma unroll
+          for (int j = 0; j < kOwn; ++j) v[j] += __uint_as_float(r[j]);
+        }
       finish_rows<kOwn>(g, v, res, bias, nw, c, 1, lane);
 #pragma unroll
       for (int j = 0; j < kOwn; ++j) res[j] = next[j];
@@ -203,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) tokens_kernel(const __grid_constant_
   }
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(MT) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
   }
 }
 
