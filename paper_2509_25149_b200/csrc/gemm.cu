@@ -889,7 +889,9 @@ cudaError_t launch_gemm_bf16_epilogue(const DenseGemmArgs& g, const EpilogueArgs
   const int pairs = num_sms / 2;
   if (e.z8_codes) {
     const int pairs_of_tile = tile == kTileSplit4 ? 4 : tile == kTileSplit2 ? 2 : 1, blocks = (g.K + 63) / 64;
-    const int share = even_share((blocks + pairs_of_tile - 1) / pairs_of_tile, code_share(g.K));
+    // Up to 256 rows 8 at most: with few tiles torch's products in binary32 take k in parts too, and are more exact (six draws of 128 x 5120 x 16384: 36 codes
+    // off, in shares of 16 / 8 152 / 84; 77.9 / 80.6 us, 256 x 5120 x 5120 28.5 / 29.0).
+    const int share = even_share((blocks + pairs_of_tile - 1) / pairs_of_tile, g.M <= 256 ? std::min(8, code_share(g.K)) : code_share(g.K));
     if (tile == kTileSplit4) return launch_bf16_epilogue<128, 4, dense::Epilogue, true>(g, e, wide, pairs, s, share);
     if (tile == kTileSplit2) return launch_bf16_epilogue<128, 2, dense::Epilogue, true>(g, e, wide, pairs, s, share);
     if (tile == kTilePair128) return launch_bf16_epilogue<128, 1, dense::Epilogue, true>(g, e, wide, pairs, s, share);

@@ -234,7 +234,7 @@ def steps_off(M, N, K, seed):
 # rows, columns, contraction, draws: one, two, three and more shares of every length, each kernel
 OFF = [(2048, 4096, K, 1) for K in (520, 776, 1024, 1096, 1536, 1608, 2048, 4096, 5120, 8200)]
 OFF += [(32, 8192, 5120, 6), (32, 8192, 16384, 6), (16, 8192, 20480, 12), (8, 20480, 4096, 12), (8, 20480, 8200, 12), (1, 20480, 20480, 40)]
-OFF += [(16, 8192, 4096, 16), (32, 8192, 4096, 12), (32, 5120, 20480, 12), (64, 8192, 4096, 8), (64, 5120, 20480, 8), (100, 8192, 4096, 6)]
+OFF += [(16, 8192, 4096, 16), (32, 8192, 4096, 12), (32, 5120, 20480, 12), (64, 8192, 4096, 8), (64, 5120, 20480, 8), (100, 8192, 4096, 6), (128, 5120, 16384, 6)]
 
 
 @pytest.mark.parametrize("M,N,K,draws", OFF)
