@@ -3,8 +3,8 @@
 //   SiLU          z s,  s = 1 / (1 + e^-z)         s + z s (1 - s)
 //   GELU          z s,  s = 1 / (1 + e^-2u)        s + z s (1 - s) 2u'       u = sqrt(2 / pi) (z + 0.044715 z^3)
 // (z/2 (1 + tanh u) is z s: the logistic form keeps its relative accuracy where z is far below zero and 1 + tanh u cancels.)
-// e^x and the quotient are the fast ones: a few units in the last place of binary32, far below the rounding to bf16 that follows (and
-// zero where 1 + e^-x is above 2^126, where the true quotient is below 2^-126).
+// e^x and the quotient are the fast ones.  The error of e^x grows with the size of its exponent, a unit in the last place of binary32 or so for each
+// unit of it: some 2^-16 of the value at 90, where it ends, far below the rounding to bf16 that follows (and zero where 1 + e^-x is above 2^126, where the true quotient is below 2^-126).
 #pragma once
 #include <cuda_runtime.h>
 

@@ -90,7 +90,7 @@ inline int even_share(int blocks, int most) {
   const int parts = (blocks + most - 1) / most;
   return (blocks + parts - 1) / parts;
 }
-// The same with sums of 1024 products at most added up outside the tensor cores (SHARE in gemm_bf16.cuh); no 512-wide tiles
+// The same with sums of 1024 products at most added up outside the tensor cores (SHARES in gemm_bf16.cuh); no 512-wide tiles
 cudaError_t launch_gemm_bf16_shares(const DenseGemmArgs& g0, const DenseGemmArgs* g1, int tile, cudaStream_t s);
 // What follows a product (nvfp4_gemm_bf16_epilogue): z = A B^T + bias, D = act(z) + residual, z kept in bf16 or as a copy in 8 bits
 struct EpilogueArgs {

@@ -6,8 +6,8 @@
 //
 // Both are bound by HBM, so a row is read once: it stays on the SM (forward: in the registers, gradient: in shared memory) of one to
 // sixteen warps, up to five chunks of eight elements a lane, between the statistic and its use, and warps of a row exchange partial sums
-// through shared memory.  Of the measured copy rate: forward of 8192 x 5120 with a bf16 residual 54.8 us (94 %), gradient from bf16 57 us
-// (90 %), from 8 bits 51 us (88 %), from and to binary32 116 us (78 %).
+// through shared memory.  Of the measured copy rate: forward of 8192 x 5120 with a bf16 residual 54.5 us (94 %), gradient from bf16 57.6 us
+// (89 %), from 8 bits 50.9 us (89 %), from and to binary32 115 us (78 %).
 #include "around.h"
 #include "copy8.cuh"
 
