@@ -246,3 +246,43 @@ def test_codes_are_about_as_exact_as_those_of_binary32_sums(M, N, K, draws):
         x, y = steps_off(M, N, K, 200 + seed)
         mine, plain = mine + x, plain + y
     assert mine <= 2.25 * plain + 4 * (mine + 2.25 ** 2 * plain) ** 0.5, (mine, plain)
+
+
+def test_products_with_codes_beside_each_other():
+    """Every kernel of the products that keep z in 8 bits, in two captured graphs that are replayed on two streams at once: the bits of direct calls."""
+    shapes = [(8, 20480, 1032), (20, 5120, 5120), (64, 2568, 5120), (100, 5128, 4104), (300, 2056, 2568), (2048, 2304, 520)]
+
+    def make(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        new = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+        calls = [(new(M, K), new(N, K), new(M, N), torch.empty((M, N), dtype=torch.bfloat16, device="cuda"), B.alloc_tensor(M, N, format=B.FORMAT_MXFP8))
+                 for M, N, K in shapes]
+
+        def step():
+            for a, b, res, D, z in calls:
+                B.nvfp4_gemm_bf16_epilogue(a, b, D, None, B.ACT_SILU, res, z)
+        return step, [t for _, _, _, D, z in calls for t in (D, z.codes, z.scales)]
+
+    both, want = [make(300), make(400)], []
+    for step, outs in both:
+        step()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in outs])
+    graphs, streams = [], [torch.cuda.Stream() for _ in both]
+    for (step, outs), stream in zip(both, streams):
+        for t in outs:
+            t.fill_(77)
+        stream.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    B.nvfp4_device_status()
+    for (_, outs), ref in zip(both, want):
+        assert all(torch.equal(a, b) for a, b in zip(outs, ref))
