@@ -206,6 +206,7 @@ def prepare(case, seed):
             s["dlogits"] = _empty(rows, wide, dtype=dtype)
         for name in ("logprob", "lse", "entropy"):
             s[name] = _empty(rows, dtype=torch.float32)
+        s["row_stats"] = _empty(rows, 2, dtype=torch.float32) if case["train"] else None
         if case["top"]:
             s["top_ids"] = _empty(rows, case["top"], dtype=torch.int32)
             s["top_logprobs"] = _empty(rows, case["top"], dtype=torch.float32)
@@ -373,15 +374,15 @@ def _library(s):
         return {"dtable": s["dtable"]}
     if kind == "logprob":
         entropy = s["entropy"] if case["entropy"] else None
-        B.nvfp4_logprob_fwd(s["logits"], s["targets"], logprob=s["logprob"], lse=s["lse"], entropy=entropy, top_ids=s.get("top_ids"),
-                            top_logprobs=s.get("top_logprobs"), scale=_scale(case))
+        B.nvfp4_logprob_fwd(s["logits"], s["targets"], logprob=s["logprob"], lse=s["lse"], stats=s["row_stats"], entropy=entropy,
+                            top_ids=s.get("top_ids"), top_logprobs=s.get("top_logprobs"), scale=_scale(case))
         out = {"lse": s["lse"], "logprob": s["logprob"]}
         if case["entropy"]:
             out["entropy"] = s["entropy"]
         if case["top"]:
             out["top_ids"], out["top_logprobs"] = s["top_ids"], s["top_logprobs"]
         if case["train"]:
-            B.nvfp4_logprob_bwd(s["logits"], s["targets"], s["lse"], s["dlogits"], dlogprob=s["dlogprob"], entropy=entropy,
+            B.nvfp4_logprob_bwd(s["logits"], s["targets"], s["row_stats"], s["dlogits"], dlogprob=s["dlogprob"], entropy=entropy,
                                 dentropy=s.get("dentropy"), scale=_scale(case))
             out["dlogits"] = s["dlogits"]
         return out
