@@ -379,6 +379,108 @@ NVFP4_API nvfp4_status nvfp4_linear_bf16_bwd8(const void* dY, const nvfp4_tensor
 NVFP4_API nvfp4_status nvfp4_dequantize_bf16(const nvfp4_tensor* t, void* out_bf16, int64_t ld, void* cuda_stream);
 
 /*
+ * The ends of a training step: what the recipe keeps in BF16 and binary32 in front of its linear layers and behind them (Section 4.1: embeddings,
+ * output head, norms), and what stands between the weight gradients and their use.  Conventions as for the operators around the layers:
+ * bf16 leading dimensions are multiples of 8, binary32 ones of 4, pointers 16-byte aligned, cols a multiple of 8, any number of rows from
+ * one on, workspaces 256-byte aligned and not shared by calls that may run at the same time, every sum in an order that depends on the
+ * sizes and the GPU alone.  Tokens, targets and positions are int32, or int64 where ..._is_int64 is set.
+ *
+ * nvfp4_headnorm_fwd: the query and key heads of a QKV product.  Row r of x [rows x (heads_q + heads_k) * head_dim] holds the query heads,
+ *   then the key heads (what stands behind them in the row, the values, is neither read nor written: ldx says where the next row begins).
+ *   Every head:  n = x / sqrt(mean(x^2) + eps),  u = n * gain (gain_q or gain_k: binary32 [head_dim], NULL: ones),  y = u rotated by the row's position p:
+ *     the first rotary_dim elements in pairs (i, i + rotary_dim / 2), or (2i, 2i + 1) where `interleaved` is set, i < rotary_dim / 2:
+ *     (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = p * inv_freq[i], a product in 64 bits;  the others stay as they are.
+ *   positions: [rows], of any sign, or NULL (0 .. rows - 1).  inv_freq: binary32 [rotary_dim / 2], NULL with rotary_dim == 0 (no rotation).
+ *   head_dim: a multiple of 8 up to 256.  rotary_dim: a multiple of 16 up to head_dim.  heads_q or heads_k may be 0.  eps > 0.
+ *   y: bf16, rounded once; may be x itself (same leading dimension).
+ * nvfp4_headnorm_bwd: with u' = dy rotated back, n from x:  dgain = (accumulate_dgain ? dgain : 0) + sum over rows and heads of u' * n,  g = u' * gain,
+ *   dx = (g - n * mean(g * n)) / sqrt(mean(x^2) + eps).  x as the forward call read it (a caller that wrote y over it keeps a copy).
+ *   dx: bf16; may be dy or x itself (same leading dimension).  dgain_q, dgain_k: NULL or binary32 [head_dim].
+ *   workspace: nvfp4_headnorm_bwd_workspace_bytes(rows, heads_q, heads_k, head_dim); NULL without dgain_q and dgain_k.
+ */
+NVFP4_API nvfp4_status nvfp4_headnorm_fwd(const void* x_bf16, int64_t ldx, int64_t rows, int32_t heads_q, int32_t heads_k,
+                                          int32_t head_dim, const float* gain_q, const float* gain_k, float eps,
+                                          const float* inv_freq, int32_t rotary_dim, int32_t interleaved, const void* positions,
+                                          int32_t positions_are_int64, void* y_bf16, int64_t ldy, void* cuda_stream);
+NVFP4_API size_t nvfp4_headnorm_bwd_workspace_bytes(int64_t rows, int32_t heads_q, int32_t heads_k, int32_t head_dim);
+NVFP4_API nvfp4_status nvfp4_headnorm_bwd(const void* dy_bf16, int64_t lddy, const void* x_bf16, int64_t ldx, int64_t rows,
+                                          int32_t heads_q, int32_t heads_k, int32_t head_dim, const float* gain_q,
+                                          const float* gain_k, float eps, const float* inv_freq, int32_t rotary_dim,
+                                          int32_t interleaved, const void* positions, int32_t positions_are_int64, void* dx_bf16,
+                                          int64_t lddx, float* dgain_q, float* dgain_k, int32_t accumulate_dgain, void* workspace,
+                                          size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * nvfp4_embedding_fwd: out[i] = scale * table[token i] (n rows of cols).  A token outside of [0, vocab) (padding) gives a row of zeros.
+ *   table: bf16 or binary32 (table_is_fp32) [vocab x cols], leading dimension ldt.  out: bf16 or binary32.
+ * nvfp4_embedding_bwd: dtable[v] = (accumulate ? dtable[v] : 0) + scale * sum of dout[i] over the i whose token is v, added in binary32 in the
+ *   order of i (in shares of that order where a token has many).  Padding adds nothing; with accumulate the rows of other tokens are not touched.
+ *   dout: bf16 or binary32 [n x cols].  dtable: binary32 [vocab x cols].
+ *   workspace: nvfp4_embedding_bwd_workspace_bytes(n, vocab, cols).
+ *   n, vocab up to 2^30.
+ */
+NVFP4_API nvfp4_status nvfp4_embedding_fwd(const void* tokens, int32_t tokens_are_int64, int64_t n, const void* table,
+                                           int32_t table_is_fp32, int64_t ldt, int64_t vocab, int64_t cols, float scale, void* out,
+                                           int32_t out_is_fp32, int64_t ldo, void* cuda_stream);
+NVFP4_API size_t nvfp4_embedding_bwd_workspace_bytes(int64_t n, int64_t vocab, int64_t cols);
+NVFP4_API nvfp4_status nvfp4_embedding_bwd(const void* tokens, int32_t tokens_are_int64, int64_t n, const void* dout,
+                                           int32_t dout_is_fp32, int64_t lddo, int64_t vocab, int64_t cols, float scale,
+                                           float* dtable, int64_t lddt, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                           void* cuda_stream);
+
+/*
+ * Log probabilities of given tokens, from logits [rows x vocab], bf16 or binary32 (logits_are_fp32); vocab is any number from one on (the
+ * leading dimension's rule stands).  A logit of minus infinity (a token that is ruled out) has probability 0; it counts as a finite input here.
+ *   z = scale * logit (2^-100 <= scale <= 2^100: one over the temperature),  lse = ln sum e^z,  log p = z - lse.
+ * nvfp4_logprob_fwd: each output may be NULL, not all.
+ *   logprob: binary32 [rows], log p of the row's target; 0 where the target is outside of [0, vocab) (padding).  Wants targets.
+ *   lse, entropy: binary32 [rows]; entropy = - sum p log p.
+ *   stats: binary32 [rows x 2], 8-byte aligned: the row's largest logit and ln sum e^(z - largest z), which nvfp4_logprob_bwd takes (lse alone
+ *   would not hold the sum beside a large logit).
+ *   top_ids (int32), top_logprobs (binary32): [rows x top], the `top` likeliest tokens, likeliest first, equal ones by index; 1 <= top <=
+ *   NVFP4_TOP_MAX and <= vocab where either is wanted.
+ *   A row of nothing but minus infinities has lse and log probabilities of minus infinity and entropy 0.
+ * nvfp4_logprob_bwd: the gradient of sum over rows of dlogprob * logprob + dentropy * entropy by the logits:
+ *   dlogits = scale * (dlogprob * ((j == target) - p) - dentropy * p * (log p + entropy)), in the type of the logits or the other one (dlogits_is_fp32),
+ *   the columns from vocab to dcols (>= vocab: what the product behind it reads) set to zero.
+ *   stats, entropy as the forward call wrote them (entropy only with dentropy).  dlogprob (with targets), dentropy: binary32 [rows], either may be NULL,
+ *   not both.  Padded targets take no part in dlogprob.  Rows of nothing but minus infinities get zeros.
+ *   dlogits may be the logits themselves (same type and leading dimension).
+ */
+#define NVFP4_TOP_MAX 32
+NVFP4_API nvfp4_status nvfp4_logprob_fwd(const void* logits, int32_t logits_are_fp32, int64_t ld, int64_t rows, int64_t vocab,
+                                         const void* targets, int32_t targets_are_int64, float scale, float* logprob, float* lse,
+                                         float* stats, float* entropy, int32_t top, int32_t* top_ids, float* top_logprobs,
+                                         void* cuda_stream);
+NVFP4_API nvfp4_status nvfp4_logprob_bwd(const void* logits, int32_t logits_are_fp32, int64_t ld, int64_t rows, int64_t vocab,
+                                         const void* targets, int32_t targets_are_int64, float scale, const float* stats,
+                                         const float* entropy, const float* dlogprob, const float* dentropy, void* dlogits,
+                                         int32_t dlogits_are_fp32, int64_t lddl, int64_t dcols, void* cuda_stream);
+
+/*
+ * The norm of many gradients, and clipping.  The list is in HOST memory and read before the call returns; tensors are contiguous, aligned to
+ * their elements, of any number of elements (0 too), and do not overlap.
+ * nvfp4_grad_sq_norm: *sum = (accumulate ? *sum : 0) + the sum of the squares of all elements, in 64 bits but for the sums of eight neighbours.  sum: DEVICE
+ *   double.  `out` is not looked at.  workspace: nvfp4_grad_sq_norm_workspace_bytes().
+ *   Data-parallel ranks that hold shares of the gradients add up their sums before the next call.
+ * nvfp4_grad_clip: norm = sqrt(*sum), factor = norm > max_norm ? max_norm / norm : 1, out = data * factor in out's type (out == NULL, or data itself in
+ *   its own type: in place, where a factor of 1 writes nothing).  Where *sum is not finite, the factor is 0 and out is zeros.
+ *   stats: NULL or DEVICE float[2], {norm, factor}.  max_norm > 0, finite.
+ */
+typedef struct nvfp4_grad {
+  void* data;        /* bf16 or binary32 */
+  void* out;         /* NULL: data */
+  int64_t count;
+  int32_t is_fp32;
+  int32_t out_is_fp32; /* heeded where out is given */
+} nvfp4_grad;
+NVFP4_API size_t nvfp4_grad_sq_norm_workspace_bytes(void);
+NVFP4_API nvfp4_status nvfp4_grad_sq_norm(const nvfp4_grad* grads, int32_t n, double* sum, int32_t accumulate, void* workspace,
+                                          size_t workspace_bytes, void* cuda_stream);
+NVFP4_API nvfp4_status nvfp4_grad_clip(const nvfp4_grad* grads, int32_t n, const double* sum, float max_norm, float* stats,
+                                       void* cuda_stream);
+
+/*
  * Test aids (not on the hot path).
  * nvfp4_dequantize: out[r][c] = code * fp32(block scale) * s_dec as fp32 (the decode of Section 2), any format.
  * nvfp4_rht16: the transformed values y = x*(S*H_16) of the row-wise (colwise == 0, out [rows x cols])

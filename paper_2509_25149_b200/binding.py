@@ -32,6 +32,9 @@ EXPORTED = (
     "nvfp4_dequantize_bf16", "nvfp4_rmsnorm_fwd", "nvfp4_rmsnorm_bwd_workspace_bytes", "nvfp4_rmsnorm_bwd",
     "nvfp4_gemm_bf16_epilogue", "nvfp4_act_bwd_workspace_bytes", "nvfp4_act_bwd", "nvfp4_linear_bf16_bwd8_workspace_bytes",
     "nvfp4_linear_bf16_bwd8",
+    "nvfp4_headnorm_fwd", "nvfp4_headnorm_bwd_workspace_bytes", "nvfp4_headnorm_bwd",
+    "nvfp4_embedding_fwd", "nvfp4_embedding_bwd_workspace_bytes", "nvfp4_embedding_bwd", "nvfp4_logprob_fwd", "nvfp4_logprob_bwd",
+    "nvfp4_grad_sq_norm_workspace_bytes", "nvfp4_grad_sq_norm", "nvfp4_grad_clip",
 )
 
 
@@ -105,6 +108,23 @@ def lib() -> ctypes.CDLL:
         for name in ("nvfp4_rmsnorm_bwd", "nvfp4_act_bwd", "nvfp4_linear_bf16_bwd8"):
             fn = getattr(L, name + "_workspace_bytes")
             fn.restype, fn.argtypes = sz, [i64, i64]
+        L.nvfp4_headnorm_fwd.restype = i32
+        L.nvfp4_headnorm_fwd.argtypes = [vp, i64, i64, i32, i32, i32, vp, vp, f32, vp, i32, i32, vp, i32, vp, i64, vp]
+        L.nvfp4_headnorm_bwd_workspace_bytes.restype, L.nvfp4_headnorm_bwd_workspace_bytes.argtypes = sz, [i64, i32, i32, i32]
+        L.nvfp4_headnorm_bwd.restype = i32
+        L.nvfp4_headnorm_bwd.argtypes = [vp, i64, vp, i64, i64, i32, i32, i32, vp, vp, f32, vp, i32, i32, vp, i32, vp, i64, vp, vp, i32, vp, sz, vp]
+        L.nvfp4_embedding_fwd.restype = i32
+        L.nvfp4_embedding_fwd.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, f32, vp, i32, i64, vp]
+        L.nvfp4_embedding_bwd_workspace_bytes.restype, L.nvfp4_embedding_bwd_workspace_bytes.argtypes = sz, [i64, i64, i64]
+        L.nvfp4_embedding_bwd.restype = i32
+        L.nvfp4_embedding_bwd.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, f32, vp, i64, i32, vp, sz, vp]
+        L.nvfp4_logprob_fwd.restype = i32
+        L.nvfp4_logprob_fwd.argtypes = [vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.nvfp4_logprob_bwd.restype = i32
+        L.nvfp4_logprob_bwd.argtypes = [vp, i32, i64, i64, i64, vp, i32, f32, vp, vp, vp, vp, vp, i32, i64, i64, vp]
+        L.nvfp4_grad_sq_norm_workspace_bytes.restype, L.nvfp4_grad_sq_norm_workspace_bytes.argtypes = sz, []
+        L.nvfp4_grad_sq_norm.restype, L.nvfp4_grad_sq_norm.argtypes = i32, [vp, i32, vp, i32, vp, sz, vp]
+        L.nvfp4_grad_clip.restype, L.nvfp4_grad_clip.argtypes = i32, [vp, i32, vp, f32, vp, vp]
         L.nvfp4_dequantize.restype, L.nvfp4_dequantize.argtypes = i32, [TP, vp, vp]
         L.nvfp4_rht16.restype, L.nvfp4_rht16.argtypes = i32, [vp, i64, i64, i64, i32, u32, vp, vp]
         L.nvfp4_e2m1_sr.restype, L.nvfp4_e2m1_sr.argtypes = i32, [vp, vp, i64, vp, vp]
@@ -358,14 +378,14 @@ def _refuse(t, what: str) -> None:
 
 
 # (The checks are written for the host's time: a call's launch takes 3 us, and an attribute of a tensor 0.1.)
-def _matrix(t: torch.Tensor, shape, device: int, dtypes=_BF16) -> int:
-    """Checks a row-major matrix on the current device and returns its leading dimension."""
+def _matrix(t: torch.Tensor, shape, device: int, dtypes=_BF16, unit: int = 1) -> int:
+    """Checks a row-major matrix on the current device and returns its leading dimension (of a single row: its columns, rounded up to `unit`)."""
     if t.shape != shape or t.dtype not in dtypes or t.get_device() != device:
         _refuse(t, f"a row-major {tuple(shape)} matrix of {dtypes}")
     ld, inner = t.stride()
     if inner != 1:
         _refuse(t, f"a row-major {tuple(shape)} matrix of {dtypes}")
-    return ld if shape[0] > 1 else shape[1]  # (a single row's stride says nothing)
+    return ld if shape[0] > 1 else -(-shape[1] // unit) * unit  # (a single row's stride says nothing)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, device: int) -> Optional[int]:
@@ -517,6 +537,188 @@ def nvfp4_linear_bf16_bwd8(dY: torch.Tensor, X8: Optional[NVFP4Tensor], W: Optio
     ws, nws = _scratch(workspace, dev)
     _check(lib().nvfp4_linear_bf16_bwd8(dY.data_ptr(), _copy8(X8, dev) if X8 is not None else None, pw, M, N, K, pdx, pdw,
                                         int(accumulate_dw), ws, nws, _stream()), "nvfp4_linear_bf16_bwd8")
+
+
+# ---- the ends of a training step ------------------------------------------------------------------------------------------
+def _indices(t: torch.Tensor, n: int, device: int, what: str):
+    """Address of n tokens, targets or positions, and whether they are int64."""
+    wide = t.dtype is torch.int64
+    if t.shape != (n,) or not (wide or t.dtype is torch.int32) or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, f"an int32 or int64 vector of {n} {what}")
+    return t.data_ptr(), wide
+
+
+def _heads(x: torch.Tensor, heads_q: int, heads_k: int, inv_freq, positions, device: int):
+    shape = x.shape
+    rows, cols = shape
+    heads = heads_q + heads_k
+    assert heads > 0 and cols % heads == 0, f"{cols} columns are not {heads_q} + {heads_k} heads of one width"
+    dim, rotary, pf, pp, wide = cols // heads, 0, 0, 0, False
+    if inv_freq is not None:
+        rotary = 2 * inv_freq.numel()
+        pf = _vector(inv_freq, rotary // 2, device)
+    if positions is not None:
+        pp, wide = _indices(positions, rows, device, "positions")
+    return shape, rows, dim, rotary, pf, pp, wide
+
+
+def nvfp4_headnorm_fwd(x: torch.Tensor, heads_q: int, heads_k: int, y: torch.Tensor, gain_q: Optional[torch.Tensor] = None,
+                       gain_k: Optional[torch.Tensor] = None, eps: float = 1e-5, inv_freq: Optional[torch.Tensor] = None,
+                       positions: Optional[torch.Tensor] = None, interleaved: bool = False) -> None:
+    """Norm, gain and rotation of the heads in x [rows x (heads_q + heads_k) * dim], the query heads first; y may be x.  Twice as many
+    elements of a head turn as inv_freq has (None: none), by positions (None: the row) times inv_freq."""
+    dev = _device()
+    shape, rows, dim, rotary, pf, pp, wide = _heads(x, heads_q, heads_k, inv_freq, positions, dev)
+    _check(lib().nvfp4_headnorm_fwd(x.data_ptr(), _matrix(x, shape, dev), rows, heads_q, heads_k, dim, _vector(gain_q, dim, dev),
+                                    _vector(gain_k, dim, dev), eps, pf, rotary, interleaved, pp, wide, y.data_ptr(),
+                                    _matrix(y, shape, dev), _stream()), "nvfp4_headnorm_fwd")
+
+
+def nvfp4_headnorm_bwd_workspace_bytes(rows: int, heads_q: int, heads_k: int, head_dim: int) -> int:
+    return int(lib().nvfp4_headnorm_bwd_workspace_bytes(rows, heads_q, heads_k, head_dim))
+
+
+def nvfp4_headnorm_bwd(dy: torch.Tensor, x: torch.Tensor, heads_q: int, heads_k: int, dx: torch.Tensor,
+                       gain_q: Optional[torch.Tensor] = None, gain_k: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                       dgain_q: Optional[torch.Tensor] = None, dgain_k: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None,
+                       positions: Optional[torch.Tensor] = None, interleaved: bool = False, accumulate_dgain: bool = False) -> None:
+    """The gradient of nvfp4_headnorm_fwd from its input x; dx may be dy or x."""
+    dev = _device()
+    shape, rows, dim, rotary, pf, pp, wide = _heads(x, heads_q, heads_k, inv_freq, positions, dev)
+    ws, nws = _scratch(workspace, dev)
+    _check(lib().nvfp4_headnorm_bwd(dy.data_ptr(), _matrix(dy, shape, dev), x.data_ptr(), _matrix(x, shape, dev), rows, heads_q, heads_k, dim,
+                                    _vector(gain_q, dim, dev), _vector(gain_k, dim, dev), eps, pf, rotary, interleaved, pp, wide,
+                                    dx.data_ptr(), _matrix(dx, shape, dev), _vector(dgain_q, dim, dev), _vector(dgain_k, dim, dev),
+                                    accumulate_dgain, ws, nws, _stream()), "nvfp4_headnorm_bwd")
+
+
+def nvfp4_embedding_fwd(tokens: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0) -> None:
+    """out[i] = scale * table[tokens[i]], zeros for a token outside of the table."""
+    dev = _device()
+    (vocab, cols), n = table.shape, tokens.shape[0]
+    pt, wide = _indices(tokens, n, dev, "tokens")
+    _check(lib().nvfp4_embedding_fwd(pt, wide, n, table.data_ptr(), table.dtype is torch.float32,
+                                     _matrix(table, table.shape, dev, _BF16_OR_FP32), vocab, cols, scale, out.data_ptr(),
+                                     out.dtype is torch.float32, _matrix(out, (n, cols), dev, _BF16_OR_FP32), _stream()),
+           "nvfp4_embedding_fwd")
+
+
+def nvfp4_embedding_bwd_workspace_bytes(n: int, vocab: int, cols: int) -> int:
+    return int(lib().nvfp4_embedding_bwd_workspace_bytes(n, vocab, cols))
+
+
+def nvfp4_embedding_bwd(tokens: torch.Tensor, dout: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+                        accumulate: bool = False) -> None:
+    """dtable (+)= scale * the sums of dout's rows by token; without accumulate all of dtable is written."""
+    dev = _device()
+    (vocab, cols), n = dtable.shape, tokens.shape[0]
+    pt, wide = _indices(tokens, n, dev, "tokens")
+    ws, nws = _scratch(workspace, dev)
+    _check(lib().nvfp4_embedding_bwd(pt, wide, n, dout.data_ptr(), dout.dtype is torch.float32, _matrix(dout, (n, cols), dev, _BF16_OR_FP32),
+                                     vocab, cols, scale, dtable.data_ptr(), _matrix(dtable, dtable.shape, dev, (torch.float32,)), accumulate,
+                                     ws, nws, _stream()), "nvfp4_embedding_bwd")
+
+
+def _row_stats(t: Optional[torch.Tensor], rows: int, device: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.shape != (rows, 2) or t.dtype is not torch.float32 or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, f"a contiguous binary32 ({rows}, 2) tensor")
+    return t.data_ptr()
+
+
+def nvfp4_logprob_fwd(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                      top_ids: Optional[torch.Tensor] = None, top_logprobs: Optional[torch.Tensor] = None, scale: float = 1.0) -> None:
+    """Log probabilities of the targets under the softmax of scale * logits, ln of the sum, entropy, and the likeliest tokens (top_ids
+    int32, top_logprobs binary32, both [rows x top]).  stats [rows x 2] is what nvfp4_logprob_bwd takes."""
+    dev = _device()
+    rows, vocab = logits.shape
+    pt, wide, top, pid, ptl = 0, False, 0, 0, 0
+    if targets is not None:
+        pt, wide = _indices(targets, rows, dev, "targets")
+    for t, dtype in ((top_ids, torch.int32), (top_logprobs, torch.float32)):
+        if t is None:
+            continue
+        if t.dim() != 2 or t.shape[0] != rows or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or top not in (0, t.shape[1]):
+            _refuse(t, f"a contiguous {dtype} ({rows}, top) tensor")
+        top = t.shape[1]
+        if dtype is torch.int32:
+            pid = t.data_ptr()
+        else:
+            ptl = t.data_ptr()
+    _check(lib().nvfp4_logprob_fwd(logits.data_ptr(), logits.dtype is torch.float32, _matrix(logits, logits.shape, dev, _BF16_OR_FP32, 8), rows,
+                                   vocab, pt, wide, scale, _vector(logprob, rows, dev), _vector(lse, rows, dev),
+                                   _row_stats(stats, rows, dev), _vector(entropy, rows, dev), top, pid, ptl, _stream()), "nvfp4_logprob_fwd")
+
+
+def nvfp4_logprob_bwd(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, dlogits: torch.Tensor,
+                      dlogprob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                      dentropy: Optional[torch.Tensor] = None, scale: float = 1.0) -> None:
+    """The gradient of sum(dlogprob * logprob + dentropy * entropy) by the logits.  dlogits may have more columns than logits, which are
+    set to zero, and may be logits itself."""
+    dev = _device()
+    rows, vocab = logits.shape
+    dcols = dlogits.shape[1]
+    pt, wide = 0, False
+    if targets is not None:
+        pt, wide = _indices(targets, rows, dev, "targets")
+    _check(lib().nvfp4_logprob_bwd(logits.data_ptr(), logits.dtype is torch.float32, _matrix(logits, logits.shape, dev, _BF16_OR_FP32, 8), rows,
+                                   vocab, pt, wide, scale, _row_stats(stats, rows, dev), _vector(entropy, rows, dev),
+                                   _vector(dlogprob, rows, dev), _vector(dentropy, rows, dev), dlogits.data_ptr(),
+                                   dlogits.dtype is torch.float32, _matrix(dlogits, (rows, dcols), dev, _BF16_OR_FP32, 8), dcols, _stream()),
+           "nvfp4_logprob_bwd")
+
+
+_GRAD_FIELDS = struct.Struct("PPqii")  # nvfp4_grad
+
+
+class GradList:
+    """Gradients (and where their clipped values go) as the C calls take them; holds the tensors."""
+
+    def __init__(self, grads, outs=None):
+        self.grads, self.outs = list(grads), list(outs) if outs is not None else None
+        assert self.grads and (self.outs is None or len(self.outs) == len(self.grads))
+        self.device = self.grads[0].get_device()
+        fields = []
+        for g, o in zip(self.grads, self.outs if self.outs is not None else self.grads):
+            for t in (g, o):
+                if t.dtype not in _BF16_OR_FP32 or t.get_device() != self.device or t.device.type != "cuda" or not t.is_contiguous():
+                    _refuse(t, "a contiguous bf16 or binary32 tensor, as the others,")
+            assert o.numel() == g.numel()
+            fields.append(_GRAD_FIELDS.pack(g.data_ptr(), o.data_ptr(), g.numel(), g.dtype is torch.float32, o.dtype is torch.float32))
+        self.n, self.packed = len(fields), b"".join(fields)
+
+
+def grad_list(grads, outs=None) -> GradList:
+    """The list that nvfp4_grad_sq_norm and nvfp4_grad_clip take, to be kept while the tensors stay where they are."""
+    return GradList(grads, outs)
+
+
+def _total(t: torch.Tensor, device: int) -> int:
+    if t.dtype is not torch.float64 or t.numel() != 1 or t.get_device() != device:
+        _refuse(t, "one binary64 number")
+    return t.data_ptr()
+
+
+def nvfp4_grad_sq_norm_workspace_bytes() -> int:
+    return int(lib().nvfp4_grad_sq_norm_workspace_bytes())
+
+
+def nvfp4_grad_sq_norm(grads: GradList, total: torch.Tensor, workspace: torch.Tensor, accumulate: bool = False) -> None:
+    """total (binary64, one number) (+)= the sum of the squares of all gradients."""
+    dev = _device()
+    assert grads.device == dev, "gradients on the current device are wanted"
+    ws, nws = _scratch(workspace, dev)
+    _check(lib().nvfp4_grad_sq_norm(grads.packed, grads.n, _total(total, dev), accumulate, ws, nws, _stream()), "nvfp4_grad_sq_norm")
+
+
+def nvfp4_grad_clip(grads: GradList, total: torch.Tensor, max_norm: float, stats: Optional[torch.Tensor] = None) -> None:
+    """Scales the gradients to a norm of max_norm where sqrt(total) is larger; stats: binary32 {norm, factor}."""
+    dev = _device()
+    assert grads.device == dev, "gradients on the current device are wanted"
+    _check(lib().nvfp4_grad_clip(grads.packed, grads.n, _total(total, dev), max_norm, _vector(stats, 2, dev), _stream()), "nvfp4_grad_clip")
 
 
 def nvfp4_rht16(x: torch.Tensor, colwise: bool, sign_mask: int) -> torch.Tensor:

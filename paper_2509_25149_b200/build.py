@@ -13,9 +13,9 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "build")
 LIB = os.path.join(PKG, "libnvfp4_b200.so")
 SOURCES = ("quantize.cu", "quantize_mx.cu", "quantize_rht.cu", "quantize_rowscale.cu", "metrics.cu", "copy8.cu", "norm.cu", "act_bwd.cu",
-           "gemm.cu", "gemm_few.cu", "api.cu", "api_around.cu")
+           "heads.cu", "embed.cu", "logprob.cu", "clip.cu", "gemm.cu", "gemm_few.cu", "api.cu", "api_around.cu", "api_ends.cu")
 HEADERS = ("common.cuh", "quantize.h", "quantize_common.cuh", "gemm.h", "tc_ptx.cuh", "async_ptx.cuh", "gemm_2cta.cuh", "gemm_wide.cuh", "gemm_bf16.cuh", "few.cuh", "gemm_tokens.cuh",
-           "tile_memo.h", "bf16_schedule.h", "copy8.cuh", "act.cuh", "around.h")
+           "tile_memo.h", "bf16_schedule.h", "copy8.cuh", "act.cuh", "around.h", "ends.h")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo",
               "-Xcompiler", "-fPIC,-fvisibility=hidden", f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}"]
 

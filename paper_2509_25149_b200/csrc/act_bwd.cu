@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, 4) act_bwd_kernel(const Args g) {
 // 32 columns to a CTA; every warp sums a share of the rows, one thread a column's shares
 template <int kShares>
 __global__ void __launch_bounds__(32 * kShares) column_sums_kernel(const float* partial, int64_t parts, int64_t cols, float* out,
-                                                                   int accumulate) {
+                                                                   int accumulate, float* out2, int64_t split) {
   griddep_wait();
   griddep_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -159,7 +159,10 @@ __global__ void __launch_bounds__(32 * kShares) column_sums_kernel(const float* 
   float total = 0.f;
 #pragma unroll
   for (int k = 0; k < kShares; ++k) total += share[k][lane];
-  out[c] = accumulate ? out[c] + total : total;
+  float* const to = c < split ? out : out2;
+  if (!to) return;
+  const int64_t at = c < split ? c : c - split;
+  to[at] = accumulate ? to[at] + total : total;
 }
 
 template <int ACT, bool Z8>
@@ -185,12 +188,13 @@ cudaError_t launch_act(const Args& k, bool z8, dim3 grid, cudaStream_t s) {
 
 int64_t act_bwd_workspace_floats(int64_t rows, int64_t cols) { return chunk_count(rows, cols) * cols; }
 
-cudaError_t launch_column_sums(const float* partial, int64_t parts, int64_t cols, float* out, bool accumulate, cudaStream_t s) {
+cudaError_t launch_column_sums(const float* partial, int64_t parts, int64_t cols, float* out, bool accumulate, cudaStream_t s, float* out2,
+                               int64_t split) {
   // the more rows, the more warps: 148 rows of 5120 columns 5.4 us with eight of them, 8 rows of 20480 1.7 us slower with 32
   const bool many = parts > 32;
   const cudaError_t e = launch_divided(kStreamingCarveout, many ? column_sums_kernel<32> : column_sums_kernel<8>,
                                        dim3((unsigned)((cols + 31) / 32)), dim3(many ? 1024 : 256), 0, s, partial, parts, cols, out,
-                                       (int)accumulate);
+                                       (int)accumulate, out2, split > 0 ? split : cols);
   count_launch();
   return e;
 }

@@ -63,7 +63,9 @@ struct ActBwd {
 int64_t act_bwd_workspace_floats(int64_t rows, int64_t cols);
 cudaError_t launch_act_bwd(const ActBwd& a, cudaStream_t s);
 
-// out[c] = (accumulate ? out[c] : 0) + sum of `parts` rows of partial sums [parts x cols], in a fixed order (act_bwd.cu)
-cudaError_t launch_column_sums(const float* partial, int64_t parts, int64_t cols, float* out, bool accumulate, cudaStream_t s);
+// out[c] = (accumulate ? out[c] : 0) + sum of `parts` rows of partial sums [parts x cols], in a fixed order (act_bwd.cu); where
+// split > 0 the columns from there on go to out2, and out or out2 may be NULL
+cudaError_t launch_column_sums(const float* partial, int64_t parts, int64_t cols, float* out, bool accumulate, cudaStream_t s,
+                               float* out2 = nullptr, int64_t split = 0);
 
 }  // namespace nvfp4
