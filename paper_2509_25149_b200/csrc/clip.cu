@@ -15,7 +15,7 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kThreads = 256, kMaxCtas = 148 * 8, kAhead = 4, kTile = kThreads * kAhead * 8;  // elements of a tile: four chunks of eight a thread
-constexpr int kList = 600;  // tensors of a launch: 32 bytes each and 4 for the tiles before them, of 32764 bytes of parameters
+constexpr int kList = 600, kShortList = 64;  // tensors of a launch: 32 bytes each and 4 for the tiles before them, of 32764 bytes of parameters
 
 struct Tensor {
   const void* data;
@@ -24,14 +24,17 @@ struct Tensor {
   int32_t head;   // elements before the first whole chunk (data is aligned to its elements only): tiles begin behind them, the first tile takes them too
   uint8_t fp32, out_fp32, vector, pad;  // vector: out's chunks are aligned as data's are
 };
+template <int N>
 struct List {
-  Tensor t[kList];
-  int32_t first[kList];  // tiles before the tensor
+  static constexpr int kMost = N;
   int32_t n, tiles;
+  int32_t first[N];  // tiles before the tensor
+  Tensor t[N];
 };
 
 // the tensor that has the tile
-__device__ __forceinline__ int find(const List& l, int tile) {
+template <class L>
+__device__ __forceinline__ int find(const L& l, int tile) {
   int lo = 0, hi = l.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -92,14 +95,15 @@ __device__ __forceinline__ double block_sum(double v, double* part) {
   return s;
 }
 
-__global__ void __launch_bounds__(kThreads) sq_norm_kernel(const __grid_constant__ List l, double* partial) {
+template <class L>
+__global__ void __launch_bounds__(kThreads) sq_norm_kernel(const __grid_constant__ L l, double* partial) {
   __shared__ double part[kThreads / 32];
   griddep_wait();
   griddep_launch_dependents();
   double sum = 0.;
   for (int tile = blockIdx.x; tile < l.tiles; tile += gridDim.x) {
-    const Tensor& t = l.t[find(l, tile)];
-    const int k = tile - l.first[&t - l.t];
+    const int at = find(l, tile), k = tile - l.first[at];
+    const Tensor& t = l.t[at];
     const int64_t first = t.head + (int64_t)k * kTile, end = min(first + kTile, t.count);
     if (k == 0 && threadIdx.x < t.head) sum += square(element(t, threadIdx.x));
     sum += t.fp32 ? tile_squares<true>(t, first, end) : tile_squares<false>(t, first, end);
@@ -152,7 +156,8 @@ __device__ __forceinline__ void scale_tile(const Tensor& t, int64_t first, int64
   }
 }
 
-__global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ List l, const double* sum, float max_norm, float* stats) {
+template <class L>
+__global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ L l, const double* sum, float max_norm, float* stats) {
   griddep_wait();
   griddep_launch_dependents();
   const double norm = sqrt(*sum);
@@ -163,9 +168,9 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
     stats[1] = factor;
   }
   for (int tile = l.tiles - 1 - (int)blockIdx.x; tile >= 0; tile -= gridDim.x) {
-    const Tensor& t = l.t[find(l, tile)];
+    const int at = find(l, tile), k = tile - l.first[at];
+    const Tensor& t = l.t[at];
     if (t.out == t.data && factor == 1.f) continue;
-    const int k = tile - l.first[&t - l.t];
     const int64_t first = t.head + (int64_t)k * kTile, end = min(first + kTile, t.count), from = k == 0 ? 0 : first;
     if (from < first) {  // (at most seven)
       if (threadIdx.x < first) {
@@ -185,11 +190,12 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
 }
 
 // The next tensors of a list, as many as a launch holds; returns how many of the list's it took
-int fill(List& l, const nvfp4_grad* grads, int n) {
+template <class L>
+int fill(L& l, const nvfp4_grad* grads, int n) {
   l.n = 0;
   int64_t tiles = 0;
   int i = 0;
-  for (; i < n && l.n < kList; ++i) {
+  for (; i < n && l.n < L::kMost; ++i) {
     const nvfp4_grad& g = grads[i];
     if (g.count == 0) continue;
     const uintptr_t size = g.is_fp32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(g.data);
@@ -211,20 +217,18 @@ int fill(List& l, const nvfp4_grad* grads, int n) {
   l.tiles = (int32_t)tiles;
   return i;
 }
-unsigned ctas_of(const List& l) { return (unsigned)std::min(l.tiles, kMaxCtas); }
+template <class L>
+unsigned ctas_of(const L& l) { return (unsigned)std::min(l.tiles, kMaxCtas); }
 
-}  // namespace
-
-size_t grad_sq_norm_workspace() { return kMaxCtas * sizeof(double); }
-
-cudaError_t launch_grad_sq_norm(const nvfp4_grad* grads, int n, double* sum, bool accumulate, double* workspace, cudaStream_t s) {
-  List l;
+template <int N>
+cudaError_t sq_norm(const nvfp4_grad* grads, int n, double* sum, bool accumulate, double* workspace, cudaStream_t s) {
+  List<N> l;
   for (int done = 0; done < n;) {
     done += fill(l, grads + done, n - done);
     if (l.tiles == 0 && done < n) continue;
     cudaError_t e;
     if (l.tiles > 0) {
-      e = launch_divided(kStreamingCarveout, sq_norm_kernel, dim3(ctas_of(l)), dim3(kThreads), 0, s, l, workspace);
+      e = launch_divided(kStreamingCarveout, sq_norm_kernel<List<N>>, dim3(ctas_of(l)), dim3(kThreads), 0, s, l, workspace);
       count_launch();
       if (e != cudaSuccess) return e;
     }
@@ -235,17 +239,29 @@ cudaError_t launch_grad_sq_norm(const nvfp4_grad* grads, int n, double* sum, boo
   }
   return cudaSuccess;
 }
-
-cudaError_t launch_grad_clip(const nvfp4_grad* grads, int n, const double* sum, float max_norm, float* stats, cudaStream_t s) {
-  List l;
+template <int N>
+cudaError_t clip(const nvfp4_grad* grads, int n, const double* sum, float max_norm, float* stats, cudaStream_t s) {
+  List<N> l;
   for (int done = 0; done < n;) {
     done += fill(l, grads + done, n - done);
     const unsigned grid = std::max(1u, ctas_of(l));  // (without an element too: stats)
-    const cudaError_t e = launch_divided(kStreamingCarveout, clip_kernel, dim3(grid), dim3(kThreads), 0, s, l, sum, max_norm, stats);
+    const cudaError_t e = launch_divided(kStreamingCarveout, clip_kernel<List<N>>, dim3(grid), dim3(kThreads), 0, s, l, sum, max_norm, stats);
     count_launch();
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
+}
+
+}  // namespace
+
+size_t grad_sq_norm_workspace() { return kMaxCtas * sizeof(double); }
+
+// (21 KB of parameters cost the host some microseconds more than 2 KB)
+cudaError_t launch_grad_sq_norm(const nvfp4_grad* grads, int n, double* sum, bool accumulate, double* workspace, cudaStream_t s) {
+  return n <= kShortList ? sq_norm<kShortList>(grads, n, sum, accumulate, workspace, s) : sq_norm<kList>(grads, n, sum, accumulate, workspace, s);
+}
+cudaError_t launch_grad_clip(const nvfp4_grad* grads, int n, const double* sum, float max_norm, float* stats, cudaStream_t s) {
+  return n <= kShortList ? clip<kShortList>(grads, n, sum, max_norm, stats, s) : clip<kList>(grads, n, sum, max_norm, stats, s);
 }
 
 }  // namespace nvfp4

@@ -76,21 +76,24 @@ struct SortShared {
   uint32_t total[kBins], base[kBins], of_warp[32];
 };
 
-__device__ __forceinline__ void fill_with_zeros(const Sort& a) {
-  const int64_t stride = (int64_t)(gridDim.x - kSortCtas) * kSortThreads, me = (int64_t)(blockIdx.x - kSortCtas) * kSortThreads + threadIdx.x;
-  const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int64_t c4 = a.cols >> 2;
-  if (a.ldt == a.cols) {
-    float4* const p = reinterpret_cast<float4*>(a.zero);
-    const int64_t all = a.vocab * c4;
-#pragma unroll 4
-    for (int64_t i = me; i < all; i += stride) __stcs(p + i, z);
-  } else {
-    for (int64_t v = me >> 5; v < a.vocab; v += stride >> 5) {
-      float4* const p = reinterpret_cast<float4*>(a.zero + v * a.ldt);
-      for (int64_t i = threadIdx.x & 31; i < c4; i += 32) __stcs(p + i, z);
-    }
+// Zeros from shared memory, a piece at a time: one instruction stores 32 KB, so that a warp keeps an SM's stores going
+constexpr int kPiece = 32768;
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void fill_with_zeros(const Sort& a, uint8_t* smem) {
+  for (int i = threadIdx.x; i < kPiece / 16; i += kSortThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+  fence_proxy_async_smem();
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  const bool packed = a.ldt == a.cols;  // one long row then
+  const int64_t rows = packed ? 1 : a.vocab, bytes = (packed ? a.vocab : 1) * a.cols * 4, per_row = (bytes + kPiece - 1) / kPiece;
+  const int64_t stride = (int64_t)(gridDim.x - kSortCtas) * 32;
+  for (int64_t p = (int64_t)(blockIdx.x - kSortCtas) * 32 + threadIdx.x; p < rows * per_row; p += stride) {
+    const int64_t r = p / per_row, at = (p - r * per_row) * kPiece;
+    bulk_store(reinterpret_cast<uint8_t*>(a.zero + r * a.ldt) + at, smem_u32(smem), (uint32_t)min((int64_t)kPiece, bytes - at));
   }
+  asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group 0;" ::: "memory");
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
@@ -99,7 +102,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
   griddep_wait();
   griddep_launch_dependents();
   if (blockIdx.x >= kSortCtas) {
-    fill_with_zeros(a);
+    fill_with_zeros(a, smem);
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x;

@@ -2,9 +2,11 @@
 //   forward   n = x / sqrt(mean(x^2) + eps),  u = n gain,  y = u turned by the angles p inv_freq
 //   gradient  u' = dy turned back;  dgain = sum of u' n;  g = u' gain;  dx = rstd (g - n mean(g n))
 // Both are bound by HBM (4 and 6 bytes an element).  A head stays within G neighbouring lanes of a warp, eight elements to a lane (so its
-// statistic takes log2 G shuffles, and the partner of a rotated element is a shuffle away), and a warp takes the heads of a row one
-// step of 32 / G heads after the other.  Sine and cosine of a row's angles are the same for all its heads: the warp makes them once,
-// the angle in 64 bits (a far position times a frequency has its last bits below binary32), and keeps them in shared memory.
+// statistic takes log2 G shuffles; both elements of a pair that turns are the same lane's: where they are half a rotation apart it takes two runs
+// of four).  A step of a warp is 32 / G heads of one kind of a row; all rows' steps stand in one line, of which every resident warp takes an equal
+// share.  What a lane is going to need comes by cp.async through a ring in shared memory in which every thread has places of its own, so that loads
+// stay in flight whatever the registers hold and over the end of a row.  Sine and cosine of a row's angles are the same for all its heads: the warp makes them once a row, the angle in 64 bits (a far position
+// times a frequency has its last bits below binary32), and keeps them in shared memory.
 #include <algorithm>
 
 #include "around.h"
@@ -15,7 +17,9 @@ namespace nvfp4 {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps, kMaxHalf = 128, kMaxCtas = 592;
+constexpr int kWarps = 8, kThreads = 32 * kWarps, kMaxHalf = 128;
+constexpr int kRing = 8;                              // steps that a warp's ring has room for
+constexpr int kFwdCtas = 148 * 3, kBwdCtas = 148 * 2;  // as many as are resident
 enum { kPlain = 0, kHalves = 1, kNeighbours = 2 };  // which elements turn together
 
 struct Args {
@@ -27,8 +31,8 @@ struct Args {
   const float* inv_freq;
   Indices positions;
   float* partial;  // gradient: a row of 2 dim sums per CTA, or NULL
-  int64_t rows, ldx, lddy, ldy, items;
-  int heads_q, heads_k, dim, half, parts, steps_per_part;
+  int64_t ldx, lddy, ldy, steps;  // steps: of all rows
+  int heads_q, heads_k, dim, half, steps_q, per_row;  // steps of a row's query heads, and of all its heads
   float eps, per_elem;
 };
 
@@ -44,51 +48,63 @@ __device__ __forceinline__ float2 turn_of(int64_t p, float f) {
 // A lane's place in a head, and its share of the row's rotation
 template <int G, int MODE>
 struct Lane {
-  int e0, partner;
+  int sub, e0, gap;  // its group's number in the warp; its elements are e0 .. e0 + 3 and e0 + gap .. e0 + gap + 3
   bool live;
-  float c[8], s[8];  // a turned element is its own times c plus its partner's times s
+  float2 c[4], s[4];  // a turned element is its own times c plus its partner's times s
   __device__ __forceinline__ Lane(const Args& a) {
-    const int lane = threadIdx.x & 31;
-    e0 = (lane % G) * 8;
-    live = e0 < a.dim;
-    partner = MODE != kHalves || e0 >= 2 * a.half ? lane : e0 < a.half ? lane + (a.half >> 3) : lane - (a.half >> 3);
+    const int l = (threadIdx.x & 31) % G;
+    sub = (threadIdx.x & 31) / G;
+    live = l * 8 < a.dim;
+    const bool apart = MODE == kHalves && l * 4 < a.half;
+    e0 = apart ? l * 4 : l * 8;
+    gap = apart ? a.half : 4;
   }
+  __device__ __forceinline__ int element(int j) const { return e0 + (j < 2 ? 2 * j : gap + 2 * j - 4); }  // of pair j
   // the warp makes the row's table in shared memory and every lane takes what it needs of it
   __device__ __forceinline__ void turn(const Args& a, float2* table, int64_t row) {
     if (MODE == kPlain) return;
     const int64_t p = a.positions.p ? a.positions[row] : row;
     for (int i = threadIdx.x & 31; i < a.half; i += 32) table[i] = turn_of(p, a.inv_freq[i]);
     __syncwarp();
+    const float2 still = make_float2(1.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float2 t = make_float2(1.f, 0.f);
-      bool first;
+    for (int j = 0; j < (MODE == kHalves ? 2 : 4); ++j) {
       if (MODE == kHalves) {
-        first = e0 < a.half;
-        if (e0 < 2 * a.half) t = table[first ? e0 + j : e0 - a.half + j];
+        const bool turns = gap != 4;  // (half a rotation is eight elements or more)
+        const float2 t = turns ? table[e0 + 2 * j] : still, u = turns ? table[e0 + 2 * j + 1] : still;
+        c[j] = c[j + 2] = make_float2(t.x, u.x);
+        s[j] = make_float2(-t.y, -u.y);
+        s[j + 2] = make_float2(t.y, u.y);
       } else {
-        first = j % 2 == 0;
-        if (e0 < 2 * a.half) t = table[(e0 + j) >> 1];
+        const float2 t = e0 < 2 * a.half ? table[(e0 >> 1) + j] : still;
+        c[j] = both(t.x);
+        s[j] = make_float2(-t.y, t.y);
       }
-      c[j] = t.x;
-      s[j] = first ? -t.y : t.y;
     }
     __syncwarp();  // (the table is the next row's)
   }
-  // what stands beside the elements of a chunk: their partners' values
-  __device__ __forceinline__ void partners(uint4 raw, float (&v)[8]) const {
-    if (MODE == kHalves) {
-      uint4 r;
-      r.x = __shfl_sync(0xffffffffu, raw.x, partner);
-      r.y = __shfl_sync(0xffffffffu, raw.y, partner);
-      r.z = __shfl_sync(0xffffffffu, raw.z, partner);
-      r.w = __shfl_sync(0xffffffffu, raw.w, partner);
-      unpack8(r, v);
-    } else if (MODE == kNeighbours) {
-      float w[8];
-      unpack8(raw, w);
+  // what stands beside the elements: their partners
+  __device__ __forceinline__ static float2 partner(const float2 (&v)[4], int j) {
+    return MODE == kHalves ? v[j ^ 2] : make_float2(v[j].y, v[j].x);
+  }
+  __device__ __forceinline__ void load_gains(const float* gain, float2 (&g)[4]) const {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = w[j ^ 1];
+    for (int j = 0; j < 4; ++j) g[j] = live && gain ? *reinterpret_cast<const float2*>(gain + element(j)) : both(1.f);
+  }
+  __device__ __forceinline__ void fetch(uint32_t dst, const uint16_t* p, bool there) const {
+    if (MODE == kHalves) {
+      copy_async<8>(dst, p, there);
+      copy_async<8>(dst + 8, p + (there ? gap : 0), there);
+    } else {
+      copy_async<16>(dst, p, there);
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* p, const float2 (&v)[4]) const {
+    if (MODE == kHalves) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0].x, v[0].y), pack2(v[1].x, v[1].y));
+      *reinterpret_cast<uint2*>(p + gap) = make_uint2(pack2(v[2].x, v[2].y), pack2(v[3].x, v[3].y));
+    } else {
+      store8<false>(p, 0, v);
     }
   }
 };
@@ -99,170 +115,233 @@ __device__ __forceinline__ float head_sum(float v) {
   for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ float dot8(const float (&a)[8], const float (&b)[8]) {
-  float2 s = make_float2(a[0] * b[0], a[1] * b[1]);
-#pragma unroll
-  for (int j = 2; j < 8; j += 2) s = fma2(make_float2(a[j], a[j + 1]), make_float2(b[j], b[j + 1]), s);
+__device__ __forceinline__ float dot8(const float2 (&a)[4], const float2 (&b)[4]) {
+  const float2 s = add2(fma2(a[1], b[1], mul2(a[0], b[0])), fma2(a[3], b[3], mul2(a[2], b[2])));
   return s.x + s.y;
 }
 // 1 / sqrt(mean(x^2) + eps) of the head that a lane's group holds.  Finite values whose squares, or the sum of them, binary32 does not hold
-// are taken times 2^-70 once more (one of them is above 2^50 then, and eps nothing beside it).
+// are taken times 2^-70 (one of them is above 2^50 then, and eps nothing beside it): `shift` says what the values have to be multiplied by before the
+// result applies to them.
 template <int G>
-__device__ __forceinline__ float rstd_of(const Args& a, const float (&x)[8]) {
-  float sum = head_sum<G>(dot8(x, x));
+__device__ __forceinline__ float rstd_of(const Args& a, const float2 (&x)[4], float& shift) {
+  const float sum = head_sum<G>(dot8(x, x));
+  shift = 1.f;
   if (__builtin_expect(__any_sync(0xffffffffu, !(sum <= 3.402823466e38f)), 0)) {
-    float w[8];
+    float2 w[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = x[j] * 0x1p-70f;
+    for (int j = 0; j < 4; ++j) w[j] = mul2(x[j], both(0x1p-70f));
     const float scaled = head_sum<G>(dot8(w, w));
-    if (!(sum <= 3.402823466e38f)) return rsqrtf(scaled * a.per_elem) * 0x1p-70f;
+    if (!(sum <= 3.402823466e38f)) {
+      shift = 0x1p-70f;
+      return rsqrtf(scaled * a.per_elem);
+    }
   }
   return rsqrtf(fmaf(sum, a.per_elem, a.eps));
 }
 
-// The steps of one kind of heads (queries, then keys) that an item has: where they begin and end
-struct Range {
-  int from, to, head0, heads;
-  __device__ __forceinline__ Range(const Args& a, int part, int kind, int per_step) {
-    const int nq = (a.heads_q + per_step - 1) / per_step, nk = (a.heads_k + per_step - 1) / per_step, begin = kind ? nq : 0;
-    const int t0 = part * a.steps_per_part, t1 = min(t0 + a.steps_per_part, nq + nk);
-    from = max(t0, begin) - begin;
-    to = min(t1, begin + (kind ? nk : nq)) - begin;
-    head0 = kind ? a.heads_q : 0;
-    heads = kind ? a.heads_k : a.heads_q;
+// Where a warp is in its share of the steps: `left` more of this kind of heads in the row, of which the lane's group has head h
+struct Walk {
+  int64_t row;
+  int key, h, left;  // key: 0 the query heads, 1 the key heads
+  __device__ __forceinline__ Walk(const Args& a, int64_t step, int per_step, int sub) : row(step / a.per_row) {
+    const int t = (int)(step - row * a.per_row);
+    key = t >= a.steps_q;
+    h = (key ? t - a.steps_q : t) * per_step + sub;
+    left = (key ? a.per_row : a.steps_q) - t;
+  }
+  __device__ __forceinline__ int heads(const Args& a) const { return key ? a.heads_k : a.heads_q; }
+  __device__ __forceinline__ int64_t offset(const Args& a, int64_t ld, int e0) const { return row * ld + (int64_t)((key ? a.heads_q : 0) + h) * a.dim + e0; }
+  // one step on; true where another kind of heads, or another row, begins
+  __device__ __forceinline__ bool next(const Args& a, int per_step, int sub) {
+    h += per_step;
+    if (--left > 0) return false;
+    h = sub;
+    if (!key && a.per_row > a.steps_q) {
+      key = 1;
+      left = a.per_row - a.steps_q;
+    } else {
+      ++row;
+      key = a.steps_q == 0;
+      left = key ? a.per_row : a.steps_q;
+    }
+    return true;
   }
 };
 
 template <int G, int MODE>
-__global__ void __launch_bounds__(kThreads) headnorm_fwd_kernel(const Args a) {
-  constexpr int kHeads = 32 / G, kAhead = 4;  // heads of a step, steps whose loads are on their way together
+__global__ void __launch_bounds__(kThreads, 3) headnorm_fwd_kernel(const Args a) {
+  constexpr int kHeads = 32 / G, kSlot = kThreads * 16;  // heads of a step, bytes of a step of all warps
   __shared__ float2 tables[kWarps][MODE == kPlain ? 1 : kMaxHalf];
-  const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  extern __shared__ __align__(16) uint8_t ring[];
+  const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int64_t first = a.steps * w / warps;
+  const int steps = (int)(a.steps * (w + 1) / warps - first), stride = kHeads * a.dim;
   Lane<G, MODE> l(a);
+  const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
+  Walk ahead(a, first, kHeads, l.sub), at = ahead;
+  const uint16_t* from = a.x + ahead.offset(a, a.ldx, l.e0);
+  uint16_t* to = a.y + at.offset(a, a.ldy, l.e0);
+  auto fetch = [&](int i) {
+    if (i < steps) {
+      const bool there = l.live && ahead.h < ahead.heads(a);
+      l.fetch(mine + (i % kRing) * kSlot, there ? from : a.x, there);
+      from += stride;
+      if (ahead.next(a, kHeads, l.sub)) from = a.x + ahead.offset(a, a.ldx, l.e0);
+    }
+    copy_commit();  // (an empty group where there is no step: the count of groups stays that of the steps)
+  };
   griddep_wait();
   griddep_launch_dependents();
-  if (item >= a.items) return;
-  const int64_t row = item / a.parts;
-  const int part = (int)(item - row * a.parts), sub = (threadIdx.x & 31) / G;
-  l.turn(a, tables[threadIdx.x >> 5], row);
-  const uint16_t* const x = a.x + row * a.ldx;
-  uint16_t* const y = a.y + row * a.ldy;
-#pragma unroll 1
-  for (int kind = 0; kind < 2; ++kind) {
-    const Range r(a, part, kind, kHeads);
-    if (r.from >= r.to) continue;
-    float gc[8], gs[8];
-    load_gain(l.live ? (kind ? a.gain_k : a.gain_q) : nullptr, l.e0, gc);
-    if (MODE != kPlain) {
+  if (steps == 0) return;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) gs[j] = (MODE == kHalves ? __shfl_sync(0xffffffffu, gc[j], l.partner) : gc[j ^ 1]) * l.s[j];
+  for (int u = 0; u < kRing - 1; ++u) fetch(u);
+  float2 gc[4], gs[4];
+  int64_t turned = -1;  // the row whose rotation the lane has
+  bool corner = true;
+  for (int i = 0; i < steps; ++i) {
+    if (corner) {
+      if (turned != at.row) l.turn(a, tables[threadIdx.x >> 5], at.row);
+      turned = at.row;
+      float2 g[4];
+      l.load_gains(at.key ? a.gain_k : a.gain_q, g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) gc[j] *= l.c[j];
-    }
-#pragma unroll 1
-    for (int t0 = r.from; t0 < r.to; t0 += kAhead) {
-      uint4 raw[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int head = (t0 + u) * kHeads + sub;
-        const bool there = l.live && t0 + u < r.to && head < r.heads;
-        raw[u] = there ? ldg128_stream(x + (int64_t)(r.head0 + head) * a.dim + l.e0) : make_uint4(0u, 0u, 0u, 0u);
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (t0 + u >= r.to) break;
-        const int head = (t0 + u) * kHeads + sub;
-        float v[8], p[8], out[8];
-        unpack8(raw[u], v);
-        const float rstd = rstd_of<G>(a, v);
-        l.partners(raw[u], p);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          out[j] = v[j] * rstd * gc[j];
-          if (MODE != kPlain) out[j] = fmaf(p[j] * rstd, gs[j], out[j]);
-        }
-        if (l.live && head < r.heads) store8<false>(y, (int64_t)(r.head0 + head) * a.dim + l.e0, out);
+      for (int j = 0; j < 4; ++j) {
+        gc[j] = MODE == kPlain ? g[j] : mul2(g[j], l.c[j]);
+        if (MODE != kPlain) gs[j] = mul2(l.partner(g, j), l.s[j]);
       }
     }
+    copy_wait<kRing - 2>();
+    float2 v[4], out[4];
+    unpack8(lds16(mine + (i % kRing) * kSlot), v);
+    fetch(i + kRing - 1);  // into the slot of the step before, whose values went into registers a turn ago
+    float shift;
+    const float rstd = rstd_of<G>(a, v, shift);
+    if (__builtin_expect(shift != 1.f, 0)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], both(shift));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      out[j] = mul2(v[j], gc[j]);
+      if (MODE != kPlain) out[j] = fma2(l.partner(v, j), gs[j], out[j]);
+      out[j] = mul2(out[j], both(rstd));
+    }
+    if (l.live && at.h < at.heads(a)) l.store(to, out);
+    to += stride;
+    corner = at.next(a, kHeads, l.sub);
+    if (corner) to = a.y + at.offset(a, a.ldy, l.e0);
   }
+  copy_wait<0>();
 }
 
-// A warp keeps the sums of its lanes' elements over all its rows and heads in registers; at the end those of a CTA are added in a fixed
+// A warp keeps the sums of its lanes' elements over all its steps in registers; at the end those of a CTA are added in a fixed
 // order and leave as a row of partial sums, which a second kernel adds.
 template <int G, int MODE>
-__global__ void __launch_bounds__(kThreads) headnorm_bwd_kernel(const Args a) {
-  constexpr int kHeads = 32 / G, kAhead = 2;
+__global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a) {
+  constexpr int kHeads = 32 / G, kSlot = kThreads * 32;
   __shared__ float2 tables[kWarps][MODE == kPlain ? 1 : kMaxHalf];
-  __shared__ float sums[kWarps][2][G * 8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / G;
+  extern __shared__ __align__(16) uint8_t ring[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + warp;
+  const int64_t first = a.steps * w / warps;
+  const int steps = (int)(a.steps * (w + 1) / warps - first), stride = kHeads * a.dim;
   Lane<G, MODE> l(a);
-  griddep_wait();
-  griddep_launch_dependents();
-  float acc[2][8] = {};
-  for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < a.items; item += (int64_t)gridDim.x * kWarps) {
-    const int64_t row = item / a.parts;
-    const int part = (int)(item - row * a.parts);
-    l.turn(a, tables[warp], row);
-    const uint16_t* const x = a.x + row * a.ldx;
-    const uint16_t* const dy = a.dy + row * a.lddy;
-    uint16_t* const dx = a.y + row * a.ldy;
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const Range r(a, part, kind, kHeads);
-      if (r.from >= r.to) continue;
-      float gain[8];
-      load_gain(l.live ? (kind ? a.gain_k : a.gain_q) : nullptr, l.e0, gain);
-#pragma unroll 1
-      for (int t0 = r.from; t0 < r.to; t0 += kAhead) {
-        uint4 rx[kAhead], rd[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int head = (t0 + u) * kHeads + sub;
-          const bool there = l.live && t0 + u < r.to && head < r.heads;
-          const int64_t at = (int64_t)(r.head0 + head) * a.dim + l.e0;
-          rx[u] = there ? ldg128_stream(x + at) : make_uint4(0u, 0u, 0u, 0u);
-          rd[u] = there ? ldg128_stream(dy + at) : make_uint4(0u, 0u, 0u, 0u);
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          if (t0 + u >= r.to) break;
-          const int head = (t0 + u) * kHeads + sub;
-          float n[8], d[8], p[8], g[8];
-          unpack8(rx[u], n);
-          unpack8(rd[u], d);
-          const float rstd = rstd_of<G>(a, n);
-          l.partners(rd[u], p);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            n[j] *= rstd;
-            if (MODE != kPlain) d[j] = fmaf(p[j], -l.s[j], d[j] * l.c[j]);
-            acc[kind][j] = fmaf(d[j], n[j], acc[kind][j]);
-            g[j] = d[j] * gain[j];
-          }
-          const float m = head_sum<G>(dot8(g, n)) * a.per_elem;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) g[j] = rstd * fmaf(-n[j], m, g[j]);
-          if (l.live && head < r.heads) store8<false>(dx, (int64_t)(r.head0 + head) * a.dim + l.e0, g);
-        }
+  const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
+  Walk ahead(a, first, kHeads, l.sub), at = ahead;
+  const uint16_t* from_x = a.x + ahead.offset(a, a.ldx, l.e0);
+  const uint16_t* from_dy = a.dy + ahead.offset(a, a.lddy, l.e0);
+  uint16_t* to = a.y + at.offset(a, a.ldy, l.e0);
+  auto fetch = [&](int i) {
+    if (i < steps) {
+      const bool there = l.live && ahead.h < ahead.heads(a);
+      l.fetch(mine + (i % kRing) * kSlot, there ? from_x : a.x, there);
+      l.fetch(mine + (i % kRing) * kSlot + kThreads * 16, there ? from_dy : a.dy, there);
+      from_x += stride;
+      from_dy += stride;
+      if (ahead.next(a, kHeads, l.sub)) {
+        from_x = a.x + ahead.offset(a, a.ldx, l.e0);
+        from_dy = a.dy + ahead.offset(a, a.lddy, l.e0);
       }
     }
+    copy_commit();
+  };
+  griddep_wait();
+  griddep_launch_dependents();
+#pragma unroll
+  for (int u = 0; u < kRing - 1; ++u) fetch(u);
+  // acc: of the kind of heads at hand; the other kind's wait in `other`
+  float2 acc[4] = {}, other[4] = {}, gain[4];
+  auto change = [&] {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 t = acc[j];
+      acc[j] = other[j];
+      other[j] = t;
+    }
+  };
+  int64_t turned = -1;
+  int key = 0;  // the kind that acc belongs to
+  bool corner = true;
+  for (int i = 0; i < steps; ++i) {
+    if (corner) {
+      if (turned != at.row) l.turn(a, tables[warp], at.row);
+      turned = at.row;
+      l.load_gains(at.key ? a.gain_k : a.gain_q, gain);
+      if (key != at.key) change();
+      key = at.key;
+    }
+    copy_wait<kRing - 2>();
+    float2 n[4], y[4], d[4], g[4];
+    unpack8(lds16(mine + (i % kRing) * kSlot), n);
+    unpack8(lds16(mine + (i % kRing) * kSlot + kThreads * 16), y);
+    fetch(i + kRing - 1);
+    float shift;
+    float rstd = rstd_of<G>(a, n, shift);
+    if (__builtin_expect(shift != 1.f, 0)) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) n[j] = mul2(n[j], both(shift));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      n[j] = mul2(n[j], both(rstd));
+      // turned back: the sines change their sign, which those of the partner's have
+      d[j] = MODE == kPlain ? y[j] : fma2(l.partner(y, j), l.partner(l.s, j), mul2(y[j], l.c[j]));
+      acc[j] = fma2(d[j], n[j], acc[j]);
+      g[j] = mul2(d[j], gain[j]);
+    }
+    rstd *= shift;
+    const float m = head_sum<G>(dot8(g, n)) * a.per_elem;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = mul2(fma2(n[j], both(-m), g[j]), both(rstd));
+    if (l.live && at.h < at.heads(a)) l.store(to, g);
+    to += stride;
+    corner = at.next(a, kHeads, l.sub);
+    if (corner) to = a.y + at.offset(a, a.ldy, l.e0);
   }
+  copy_wait<0>();
   if (!a.partial) return;
+  if (key) change();
+  __syncthreads();  // the ring is empty; the sums take its place
+  auto sums = reinterpret_cast<float(*)[2][256]>(ring);
+  static_assert(kWarps * 2 * 256 * 4 <= kRing * kSlot, "the sums reuse the ring");
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float v = acc[kind][j];
+    for (int j = 0; j < 4; ++j) {
+      float2 v = kind ? other[j] : acc[j];
 #pragma unroll
-      for (int o = G; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane < G) sums[warp][kind][l.e0 + j] = v;
+      for (int o = G; o < 32; o <<= 1) {
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+      }
+      if (lane < G && l.live) *reinterpret_cast<float2*>(&sums[warp][kind][l.element(j)]) = v;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.dim; i += kThreads) {
     const int kind = i >= a.dim, e = i - kind * a.dim;
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) v += sums[w][kind][e];
+    for (int k = 0; k < kWarps; ++k) v += sums[k][kind][e];
     a.partial[(int64_t)blockIdx.x * 2 * a.dim + i] = v;
   }
 }
@@ -272,21 +351,13 @@ int lanes_of(int dim) {
   while (g * 8 < dim) g *= 2;
   return g;
 }
-// Items of a row: as many as give every SM two CTAs where the rows alone do not
-struct Split {
-  int parts, per_part;
-  int64_t items;
-  Split(int64_t rows, int heads_q, int heads_k, int dim) {
-    const int per_step = 32 / lanes_of(dim), steps = (heads_q + per_step - 1) / per_step + (heads_k + per_step - 1) / per_step;
-    const int64_t want = std::max<int64_t>(1, (2 * 148 * kWarps + rows - 1) / rows);
-    per_part = (int)((steps + std::min<int64_t>(want, steps) - 1) / std::min<int64_t>(want, steps));
-    parts = (steps + per_part - 1) / per_part;
-    items = rows * parts;
-  }
-};
-int64_t bwd_ctas(int64_t items) { return std::min<int64_t>((items + kWarps - 1) / kWarps, kMaxCtas); }
+int64_t steps_of_row(int heads_q, int heads_k, int dim) {
+  const int per_step = 32 / lanes_of(dim);
+  return (heads_q + per_step - 1) / per_step + (heads_k + per_step - 1) / per_step;
+}
+unsigned ctas_of(int64_t steps, int most) { return (unsigned)std::min<int64_t>((steps + kWarps - 1) / kWarps, most); }
 
-Args args_of(const Heads& h, const Split& split) {
+Args args_of(const Heads& h) {
   Args a{};
   a.x = static_cast<const uint16_t*>(h.x);
   a.dy = static_cast<const uint16_t*>(h.dy);
@@ -294,33 +365,45 @@ Args args_of(const Heads& h, const Split& split) {
   a.gain_q = h.gain_q; a.gain_k = h.gain_k;
   a.inv_freq = h.inv_freq;
   a.positions = h.positions;
-  a.rows = h.rows; a.ldx = h.ldx; a.lddy = h.lddy; a.ldy = h.ldy;
-  a.items = split.items; a.parts = split.parts; a.steps_per_part = split.per_part;
+  a.ldx = h.ldx; a.lddy = h.lddy; a.ldy = h.ldy;
   a.heads_q = h.heads_q; a.heads_k = h.heads_k;
   a.dim = h.dim; a.half = h.rotary / 2;
+  a.steps_q = (int)steps_of_row(h.heads_q, 0, h.dim);
+  a.per_row = (int)steps_of_row(h.heads_q, h.heads_k, h.dim);
+  a.steps = h.rows * a.per_row;
   a.eps = h.eps; a.per_elem = 1.f / (float)h.dim;
   return a;
 }
 
 template <int G, int MODE>
-cudaError_t launch(bool bwd, const Args& a, unsigned grid, cudaStream_t s) {
-  return bwd ? launch_divided(15, headnorm_bwd_kernel<G, MODE>, dim3(grid), dim3(kThreads), 0, s, a)
-             : launch_divided(15, headnorm_fwd_kernel<G, MODE>, dim3(grid), dim3(kThreads), 0, s, a);
+cudaError_t launch(bool bwd, const Args& a, cudaStream_t s) {
+  const auto kern = bwd ? headnorm_bwd_kernel<G, MODE> : headnorm_fwd_kernel<G, MODE>;
+  const int smem = kRing * kThreads * (bwd ? 32 : 16);
+  if (bwd) {
+    static std::atomic<uint64_t> configured{0};  // per instantiation and device
+    int dev;
+    if (device_needs_config(configured, &dev)) {
+      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e != cudaSuccess) return e;
+      device_configured(configured, dev);
+    }
+  }
+  return launch_divided(100, kern, dim3(ctas_of(a.steps, bwd ? kBwdCtas : kFwdCtas)), dim3(kThreads), smem, s, a);
 }
 template <int G>
-cudaError_t launch(bool bwd, bool interleaved, const Args& a, unsigned grid, cudaStream_t s) {
-  if (a.half == 0) return launch<G, kPlain>(bwd, a, grid, s);
-  return interleaved ? launch<G, kNeighbours>(bwd, a, grid, s) : launch<G, kHalves>(bwd, a, grid, s);
+cudaError_t launch(bool bwd, bool interleaved, const Args& a, cudaStream_t s) {
+  if (a.half == 0) return launch<G, kPlain>(bwd, a, s);
+  return interleaved ? launch<G, kNeighbours>(bwd, a, s) : launch<G, kHalves>(bwd, a, s);
 }
-cudaError_t launch(bool bwd, bool interleaved, const Args& a, unsigned grid, cudaStream_t s) {
+cudaError_t launch(bool bwd, bool interleaved, const Args& a, cudaStream_t s) {
   cudaError_t e;
   switch (lanes_of(a.dim)) {
-    case 1: e = launch<1>(bwd, interleaved, a, grid, s); break;
-    case 2: e = launch<2>(bwd, interleaved, a, grid, s); break;
-    case 4: e = launch<4>(bwd, interleaved, a, grid, s); break;
-    case 8: e = launch<8>(bwd, interleaved, a, grid, s); break;
-    case 16: e = launch<16>(bwd, interleaved, a, grid, s); break;
-    default: e = launch<32>(bwd, interleaved, a, grid, s); break;
+    case 1: e = launch<1>(bwd, interleaved, a, s); break;
+    case 2: e = launch<2>(bwd, interleaved, a, s); break;
+    case 4: e = launch<4>(bwd, interleaved, a, s); break;
+    case 8: e = launch<8>(bwd, interleaved, a, s); break;
+    case 16: e = launch<16>(bwd, interleaved, a, s); break;
+    default: e = launch<32>(bwd, interleaved, a, s); break;
   }
   count_launch();
   return e;
@@ -328,24 +411,19 @@ cudaError_t launch(bool bwd, bool interleaved, const Args& a, unsigned grid, cud
 
 }  // namespace
 
-cudaError_t launch_headnorm_fwd(const Heads& h, cudaStream_t s) {
-  const Split split(h.rows, h.heads_q, h.heads_k, h.dim);
-  return launch(false, h.interleaved, args_of(h, split), (unsigned)((split.items + kWarps - 1) / kWarps), s);
-}
+cudaError_t launch_headnorm_fwd(const Heads& h, cudaStream_t s) { return launch(false, h.interleaved, args_of(h), s); }
 
 int64_t headnorm_bwd_workspace_floats(int64_t rows, int heads_q, int heads_k, int dim) {
-  return bwd_ctas(Split(rows, heads_q, heads_k, dim).items) * 2 * dim;
+  return (int64_t)ctas_of(rows * steps_of_row(heads_q, heads_k, dim), kBwdCtas) * 2 * dim;
 }
 
 cudaError_t launch_headnorm_bwd(const Heads& h, cudaStream_t s) {
-  const Split split(h.rows, h.heads_q, h.heads_k, h.dim);
-  Args a = args_of(h, split);
+  Args a = args_of(h);
   const bool sums = h.dgain_q || h.dgain_k;
   a.partial = sums ? h.workspace : nullptr;
-  const int64_t ctas = bwd_ctas(split.items);
-  const cudaError_t e = launch(true, h.interleaved, a, (unsigned)ctas, s);
+  const cudaError_t e = launch(true, h.interleaved, a, s);
   if (e != cudaSuccess || !sums) return e;
-  return launch_column_sums(h.workspace, ctas, 2 * h.dim, h.dgain_q, h.accumulate, s, h.dgain_k, h.dim);
+  return launch_column_sums(h.workspace, ctas_of(a.steps, kBwdCtas), 2 * h.dim, h.dgain_q, h.accumulate, s, h.dgain_k, h.dim);
 }
 
 }  // namespace nvfp4
