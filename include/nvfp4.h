@@ -391,7 +391,7 @@ NVFP4_API nvfp4_status nvfp4_dequantize_bf16(const nvfp4_tensor* t, void* out_bf
  *     the first rotary_dim elements in pairs (i, i + rotary_dim / 2), or (2i, 2i + 1) where `interleaved` is set, i < rotary_dim / 2:
  *     (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = p * inv_freq[i], a product in 64 bits;  the others stay as they are.
  *   positions: [rows], of any sign, or NULL (0 .. rows - 1).  inv_freq: binary32 [rotary_dim / 2], NULL with rotary_dim == 0 (no rotation).
- *   head_dim: a multiple of 8 up to 256.  rotary_dim: a multiple of 16 up to head_dim.  heads_q or heads_k may be 0.  eps > 0.
+ *   head_dim: a multiple of 8 up to 256.  rotary_dim: a multiple of 16 up to head_dim.  heads_q or heads_k may be 0.  eps: a normal number above 0.
  *   y: bf16, rounded once; may be x itself (same leading dimension).
  * nvfp4_headnorm_bwd: with u' = dy rotated back, n from x:  dgain = (accumulate_dgain ? dgain : 0) + sum over rows and heads of u' * n,  g = u' * gain,
  *   dx = (g - n * mean(g * n)) / sqrt(mean(x^2) + eps).  x as the forward call read it (a caller that wrote y over it keeps a copy).

@@ -32,7 +32,7 @@ bool head_sizes_ok(int64_t rows, int32_t heads_q, int32_t heads_k, int32_t dim) 
 nvfp4_status check_heads(const Heads& h, const void* positions) {
   if (!h.x || !h.y || (h.rotary != 0 && !h.inv_freq)) return NVFP4_ERR_NULL;
   if (!head_sizes_ok(h.rows, h.heads_q, h.heads_k, h.dim) || h.rotary < 0 || h.rotary > h.dim || h.rotary % 16 != 0) return NVFP4_ERR_SHAPE;
-  if (!(h.eps > 0.f) || !std::isfinite(h.eps)) return NVFP4_ERR_ARG;
+  if (!(h.eps >= 0x1p-126f) || !std::isfinite(h.eps)) return NVFP4_ERR_ARG;
   const int64_t cols = (int64_t)(h.heads_q + h.heads_k) * h.dim;
   nvfp4_status st;
   if ((st = check_matrix(h.x, h.ldx, cols, false)) != NVFP4_OK || (st = check_matrix(h.y, h.ldy, cols, false)) != NVFP4_OK) return st;

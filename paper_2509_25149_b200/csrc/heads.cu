@@ -3,7 +3,8 @@
 //   gradient  u' = dy turned back;  dgain = sum of u' n;  g = u' gain;  dx = rstd (g - n mean(g n))
 // Both are bound by HBM (4 and 6 bytes an element).  A head stays within G neighbouring lanes of a warp, eight elements to a lane (so its
 // statistic takes log2 G shuffles; both elements of a pair that turns are the same lane's: where they are half a rotation apart it takes two runs
-// of four).  A step of a warp is 32 / G heads of one kind of a row; all rows' steps stand in one line, of which every resident warp takes an equal
+// of four).  A step of a warp is 32 / G or twice as many heads of one kind of a row (two heads to a lane halve what a step costs beside its arithmetic,
+// and their statistics do not wait for each other); all rows' steps stand in one line, of which every resident warp takes an equal
 // share.  What a lane is going to need comes by cp.async through a ring in shared memory in which every thread has places of its own, so that loads
 // stay in flight whatever the registers hold and over the end of a row.  Sine and cosine of a row's angles are the same for all its heads: the warp makes them once a row, the angle in 64 bits (a far position
 // times a frequency has its last bits below binary32), and keeps them in shared memory.
@@ -18,8 +19,11 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps, kMaxHalf = 128;
-constexpr int kRing = 8;                              // steps that a warp's ring has room for
-constexpr int kFwdCtas = 148 * 3, kBwdCtas = 148 * 2;  // as many as are resident
+template <int N>
+constexpr int kFwdRing = 8;  // steps that a warp's ring has room for, with N heads to a lane
+template <int N>
+constexpr int kBwdRing = N == 2 ? 4 : 8;
+constexpr int kFwdCtas = 148 * 2, kBwdCtas = 148 * 2;  // as many as are resident
 enum { kPlain = 0, kHalves = 1, kNeighbours = 2 };  // which elements turn together
 
 struct Args {
@@ -119,24 +123,44 @@ __device__ __forceinline__ float dot8(const float2 (&a)[4], const float2 (&b)[4]
   const float2 s = add2(fma2(a[1], b[1], mul2(a[0], b[0])), fma2(a[3], b[3], mul2(a[2], b[2])));
   return s.x + s.y;
 }
-// 1 / sqrt(mean(x^2) + eps) of the head that a lane's group holds.  Finite values whose squares, or the sum of them, binary32 does not hold
-// are taken times 2^-70 (one of them is above 2^50 then, and eps nothing beside it): `shift` says what the values have to be multiplied by before the
-// result applies to them.
-template <int G>
-__device__ __forceinline__ float rstd_of(const Args& a, const float2 (&x)[4], float& shift) {
-  const float sum = head_sum<G>(dot8(x, x));
-  shift = 1.f;
-  if (__builtin_expect(__any_sync(0xffffffffu, !(sum <= 3.402823466e38f)), 0)) {
+__device__ __forceinline__ float rsqrt_fast(float v) {  // (of normal numbers: eps is one at least)
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// 1 / sqrt(mean(x^2) + eps) of the N heads that a lane's group holds.  Finite values whose squares, or the sum of them, binary32 does not hold
+// are multiplied by 2^-70 (one of them is above 2^50 then, and eps nothing beside it), and the result is that of what they are now; `shift` says so.  True where the
+// warp had such a head.
+template <int G, int N>
+__device__ __forceinline__ bool rstd_of(const Args& a, float2 (&x)[N][4], float (&rstd)[N], float (*shift)[N] = nullptr) {
+  float sum[N];
+  bool lost = false;
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum[k] = dot8(x[k], x[k]);
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    lost |= !(sum[k] <= 3.402823466e38f);
+    rstd[k] = rsqrt_fast(fmaf(sum[k], a.per_elem, a.eps));
+  }
+  if (__builtin_expect(!__any_sync(0xffffffffu, lost), 1)) return false;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const bool far = !(sum[k] <= 3.402823466e38f);
     float2 w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = mul2(x[j], both(0x1p-70f));
+    for (int j = 0; j < 4; ++j) w[j] = mul2(x[k][j], both(0x1p-70f));
     const float scaled = head_sum<G>(dot8(w, w));
-    if (!(sum <= 3.402823466e38f)) {
-      shift = 0x1p-70f;
-      return rsqrtf(scaled * a.per_elem);
-    }
+    if (!far) continue;
+    rstd[k] = rsqrt_fast(scaled * a.per_elem);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[k][j] = w[j];
+    if (shift) (*shift)[k] = 0x1p-70f;
   }
-  return rsqrtf(fmaf(sum, a.per_elem, a.eps));
+  return true;
 }
 
 // Where a warp is in its share of the steps: `left` more of this kind of heads in the row, of which the lane's group has head h
@@ -168,25 +192,28 @@ struct Walk {
   }
 };
 
-template <int G, int MODE>
-__global__ void __launch_bounds__(kThreads, 3) headnorm_fwd_kernel(const Args a) {
-  constexpr int kHeads = 32 / G, kSlot = kThreads * 16;  // heads of a step, bytes of a step of all warps
+template <int G, int MODE, int N>
+__global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a) {
+  constexpr int kHeads = 32 / G, kStep = kHeads * N, kRing = kFwdRing<N>, kSlot = kThreads * 16 * N;  // heads of a step, bytes of a step of all warps
   __shared__ float2 tables[kWarps][MODE == kPlain ? 1 : kMaxHalf];
   extern __shared__ __align__(16) uint8_t ring[];
   const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int64_t first = a.steps * w / warps;
-  const int steps = (int)(a.steps * (w + 1) / warps - first), stride = kHeads * a.dim;
+  const int steps = (int)(a.steps * (w + 1) / warps - first), head = kHeads * a.dim;  // head: from a lane's first one to its second
   Lane<G, MODE> l(a);
   const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
-  Walk ahead(a, first, kHeads, l.sub), at = ahead;
+  Walk ahead(a, first, kStep, l.sub), at = ahead;
   const uint16_t* from = a.x + ahead.offset(a, a.ldx, l.e0);
   uint16_t* to = a.y + at.offset(a, a.ldy, l.e0);
   auto fetch = [&](int i) {
     if (i < steps) {
-      const bool there = l.live && ahead.h < ahead.heads(a);
-      l.fetch(mine + (i % kRing) * kSlot, there ? from : a.x, there);
-      from += stride;
-      if (ahead.next(a, kHeads, l.sub)) from = a.x + ahead.offset(a, a.ldx, l.e0);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const bool there = l.live && ahead.h + k * kHeads < ahead.heads(a);
+        l.fetch(mine + (i % kRing) * kSlot + k * (kThreads * 16), there ? from + k * head : a.x, there);
+      }
+      from += N * head;
+      if (ahead.next(a, kStep, l.sub)) from = a.x + ahead.offset(a, a.ldx, l.e0);
     }
     copy_commit();  // (an empty group where there is no step: the count of groups stays that of the steps)
   };
@@ -211,24 +238,25 @@ __global__ void __launch_bounds__(kThreads, 3) headnorm_fwd_kernel(const Args a)
       }
     }
     copy_wait<kRing - 2>();
-    float2 v[4], out[4];
-    unpack8(lds16(mine + (i % kRing) * kSlot), v);
+    float2 v[N][4];
+    float rstd[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) unpack8(lds16(mine + (i % kRing) * kSlot + k * (kThreads * 16)), v[k]);
     fetch(i + kRing - 1);  // into the slot of the step before, whose values went into registers a turn ago
-    float shift;
-    const float rstd = rstd_of<G>(a, v, shift);
-    if (__builtin_expect(shift != 1.f, 0)) {
+    rstd_of<G, N>(a, v, rstd);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], both(shift));
-    }
+    for (int k = 0; k < N; ++k) {
+      float2 out[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      out[j] = mul2(v[j], gc[j]);
-      if (MODE != kPlain) out[j] = fma2(l.partner(v, j), gs[j], out[j]);
-      out[j] = mul2(out[j], both(rstd));
+      for (int j = 0; j < 4; ++j) {
+        out[j] = mul2(v[k][j], gc[j]);
+        if (MODE != kPlain) out[j] = fma2(l.partner(v[k], j), gs[j], out[j]);
+        out[j] = mul2(out[j], both(rstd[k]));
+      }
+      if (l.live && at.h + k * kHeads < at.heads(a)) l.store(to + k * head, out);
     }
-    if (l.live && at.h < at.heads(a)) l.store(to, out);
-    to += stride;
-    corner = at.next(a, kHeads, l.sub);
+    to += N * head;
+    corner = at.next(a, kStep, l.sub);
     if (corner) to = a.y + at.offset(a, a.ldy, l.e0);
   }
   copy_wait<0>();
@@ -236,29 +264,33 @@ __global__ void __launch_bounds__(kThreads, 3) headnorm_fwd_kernel(const Args a)
 
 // A warp keeps the sums of its lanes' elements over all its steps in registers; at the end those of a CTA are added in a fixed
 // order and leave as a row of partial sums, which a second kernel adds.
-template <int G, int MODE>
+template <int G, int MODE, int N>
 __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a) {
-  constexpr int kHeads = 32 / G, kSlot = kThreads * 32;
+  constexpr int kHeads = 32 / G, kStep = kHeads * N, kRing = kBwdRing<N>, kSlot = kThreads * 32 * N;
   __shared__ float2 tables[kWarps][MODE == kPlain ? 1 : kMaxHalf];
   extern __shared__ __align__(16) uint8_t ring[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + warp;
   const int64_t first = a.steps * w / warps;
-  const int steps = (int)(a.steps * (w + 1) / warps - first), stride = kHeads * a.dim;
+  const int steps = (int)(a.steps * (w + 1) / warps - first), head = kHeads * a.dim;
   Lane<G, MODE> l(a);
   const uint32_t mine = smem_u32(ring) + threadIdx.x * 16;
-  Walk ahead(a, first, kHeads, l.sub), at = ahead;
+  Walk ahead(a, first, kStep, l.sub), at = ahead;
   const uint16_t* from_x = a.x + ahead.offset(a, a.ldx, l.e0);
   const uint16_t* from_dy = a.dy + ahead.offset(a, a.lddy, l.e0);
   uint16_t* to = a.y + at.offset(a, a.ldy, l.e0);
   auto fetch = [&](int i) {
     if (i < steps) {
-      const bool there = l.live && ahead.h < ahead.heads(a);
-      l.fetch(mine + (i % kRing) * kSlot, there ? from_x : a.x, there);
-      l.fetch(mine + (i % kRing) * kSlot + kThreads * 16, there ? from_dy : a.dy, there);
-      from_x += stride;
-      from_dy += stride;
-      if (ahead.next(a, kHeads, l.sub)) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const bool there = l.live && ahead.h + k * kHeads < ahead.heads(a);
+        const uint32_t dst = mine + (i % kRing) * kSlot + k * (kThreads * 32);
+        l.fetch(dst, there ? from_x + k * head : a.x, there);
+        l.fetch(dst + kThreads * 16, there ? from_dy + k * head : a.dy, there);
+      }
+      from_x += N * head;
+      from_dy += N * head;
+      if (ahead.next(a, kStep, l.sub)) {
         from_x = a.x + ahead.offset(a, a.ldx, l.e0);
         from_dy = a.dy + ahead.offset(a, a.lddy, l.e0);
       }
@@ -291,31 +323,46 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a)
       key = at.key;
     }
     copy_wait<kRing - 2>();
-    float2 n[4], y[4], d[4], g[4];
-    unpack8(lds16(mine + (i % kRing) * kSlot), n);
-    unpack8(lds16(mine + (i % kRing) * kSlot + kThreads * 16), y);
+    float2 n[N][4], y[N][4];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const uint32_t src = mine + (i % kRing) * kSlot + k * (kThreads * 32);
+      unpack8(lds16(src), n[k]);
+      unpack8(lds16(src + kThreads * 16), y[k]);
+    }
     fetch(i + kRing - 1);
-    float shift;
-    float rstd = rstd_of<G>(a, n, shift);
-    if (__builtin_expect(shift != 1.f, 0)) {
+    float rstd[N], m[N], shift[N];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) n[j] = mul2(n[j], both(shift));
+    for (int k = 0; k < N; ++k) shift[k] = 1.f;
+    const bool far = rstd_of<G, N>(a, n, rstd, &shift);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      float2 g[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        n[k][j] = mul2(n[k][j], both(rstd[k]));
+        // turned back: the sines change their sign, which those of the partner's have
+        g[j] = MODE == kPlain ? y[k][j] : fma2(l.partner(y[k], j), l.partner(l.s, j), mul2(y[k][j], l.c[j]));
+        acc[j] = fma2(g[j], n[k][j], acc[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[k][j] = mul2(g[j], gain[j]);
+      m[k] = dot8(y[k], n[k]);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      n[j] = mul2(n[j], both(rstd));
-      // turned back: the sines change their sign, which those of the partner's have
-      d[j] = MODE == kPlain ? y[j] : fma2(l.partner(y, j), l.partner(l.s, j), mul2(y[j], l.c[j]));
-      acc[j] = fma2(d[j], n[j], acc[j]);
-      g[j] = mul2(d[j], gain[j]);
-    }
-    rstd *= shift;
-    const float m = head_sum<G>(dot8(g, n)) * a.per_elem;
+    for (int o = G / 2; o > 0; o >>= 1)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) g[j] = mul2(fma2(n[j], both(-m), g[j]), both(rstd));
-    if (l.live && at.h < at.heads(a)) l.store(to, g);
-    to += stride;
-    corner = at.next(a, kHeads, l.sub);
+      for (int k = 0; k < N; ++k) m[k] += __shfl_xor_sync(0xffffffffu, m[k], o);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float r = far ? rstd[k] * shift[k] : rstd[k];
+      float2 out[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) out[j] = mul2(fma2(n[k][j], both(-m[k] * a.per_elem), y[k][j]), both(r));
+      if (l.live && at.h + k * kHeads < at.heads(a)) l.store(to + k * head, out);
+    }
+    to += N * head;
+    corner = at.next(a, kStep, l.sub);
     if (corner) to = a.y + at.offset(a, a.ldy, l.e0);
   }
   copy_wait<0>();
@@ -351,13 +398,16 @@ int lanes_of(int dim) {
   while (g * 8 < dim) g *= 2;
   return g;
 }
-int64_t steps_of_row(int heads_q, int heads_k, int dim) {
+int64_t steps_of_row(int heads_q, int heads_k, int per_step) { return (heads_q + per_step - 1) / per_step + (heads_k + per_step - 1) / per_step; }
+// Two heads to a lane unless more than an eighth of the places would be empty for it
+int heads_of_lane(int heads_q, int heads_k, int dim) {
   const int per_step = 32 / lanes_of(dim);
-  return (heads_q + per_step - 1) / per_step + (heads_k + per_step - 1) / per_step;
+  return 8 * 2 * steps_of_row(heads_q, heads_k, 2 * per_step) <= 9 * steps_of_row(heads_q, heads_k, per_step) ? 2 : 1;
 }
+int64_t steps_of_row(int heads_q, int heads_k, int dim, int n) { return steps_of_row(heads_q, heads_k, n * (32 / lanes_of(dim))); }
 unsigned ctas_of(int64_t steps, int most) { return (unsigned)std::min<int64_t>((steps + kWarps - 1) / kWarps, most); }
 
-Args args_of(const Heads& h) {
+Args args_of(const Heads& h, int n) {
   Args a{};
   a.x = static_cast<const uint16_t*>(h.x);
   a.dy = static_cast<const uint16_t*>(h.dy);
@@ -368,42 +418,44 @@ Args args_of(const Heads& h) {
   a.ldx = h.ldx; a.lddy = h.lddy; a.ldy = h.ldy;
   a.heads_q = h.heads_q; a.heads_k = h.heads_k;
   a.dim = h.dim; a.half = h.rotary / 2;
-  a.steps_q = (int)steps_of_row(h.heads_q, 0, h.dim);
-  a.per_row = (int)steps_of_row(h.heads_q, h.heads_k, h.dim);
+  a.steps_q = (int)steps_of_row(h.heads_q, 0, h.dim, n);
+  a.per_row = (int)steps_of_row(h.heads_q, h.heads_k, h.dim, n);
   a.steps = h.rows * a.per_row;
   a.eps = h.eps; a.per_elem = 1.f / (float)h.dim;
   return a;
 }
 
-template <int G, int MODE>
+template <int G, int MODE, int N>
 cudaError_t launch(bool bwd, const Args& a, cudaStream_t s) {
-  const auto kern = bwd ? headnorm_bwd_kernel<G, MODE> : headnorm_fwd_kernel<G, MODE>;
-  const int smem = kRing * kThreads * (bwd ? 32 : 16);
-  if (bwd) {
-    static std::atomic<uint64_t> configured{0};  // per instantiation and device
-    int dev;
-    if (device_needs_config(configured, &dev)) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      if (e != cudaSuccess) return e;
-      device_configured(configured, dev);
-    }
+  const auto kern = bwd ? headnorm_bwd_kernel<G, MODE, N> : headnorm_fwd_kernel<G, MODE, N>;
+  const int smem = kThreads * N * (bwd ? kBwdRing<N> * 32 : kFwdRing<N> * 16);
+  static std::atomic<uint64_t> configured[2]{};  // per instantiation and device
+  int dev;
+  if (device_needs_config(configured[bwd], &dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    device_configured(configured[bwd], dev);
   }
   return launch_divided(100, kern, dim3(ctas_of(a.steps, bwd ? kBwdCtas : kFwdCtas)), dim3(kThreads), smem, s, a);
 }
-template <int G>
-cudaError_t launch(bool bwd, bool interleaved, const Args& a, cudaStream_t s) {
-  if (a.half == 0) return launch<G, kPlain>(bwd, a, s);
-  return interleaved ? launch<G, kNeighbours>(bwd, a, s) : launch<G, kHalves>(bwd, a, s);
+template <int G, int MODE>
+cudaError_t launch(bool bwd, int n, const Args& a, cudaStream_t s) {
+  return n == 2 ? launch<G, MODE, 2>(bwd, a, s) : launch<G, MODE, 1>(bwd, a, s);
 }
-cudaError_t launch(bool bwd, bool interleaved, const Args& a, cudaStream_t s) {
+template <int G>
+cudaError_t launch(bool bwd, bool interleaved, int n, const Args& a, cudaStream_t s) {
+  if (a.half == 0) return launch<G, kPlain>(bwd, n, a, s);
+  return interleaved ? launch<G, kNeighbours>(bwd, n, a, s) : launch<G, kHalves>(bwd, n, a, s);
+}
+cudaError_t launch(bool bwd, bool interleaved, int n, const Args& a, cudaStream_t s) {
   cudaError_t e;
   switch (lanes_of(a.dim)) {
-    case 1: e = launch<1>(bwd, interleaved, a, s); break;
-    case 2: e = launch<2>(bwd, interleaved, a, s); break;
-    case 4: e = launch<4>(bwd, interleaved, a, s); break;
-    case 8: e = launch<8>(bwd, interleaved, a, s); break;
-    case 16: e = launch<16>(bwd, interleaved, a, s); break;
-    default: e = launch<32>(bwd, interleaved, a, s); break;
+    case 1: e = launch<1>(bwd, interleaved, n, a, s); break;
+    case 2: e = launch<2>(bwd, interleaved, n, a, s); break;
+    case 4: e = launch<4>(bwd, interleaved, n, a, s); break;
+    case 8: e = launch<8>(bwd, interleaved, n, a, s); break;
+    case 16: e = launch<16>(bwd, interleaved, n, a, s); break;
+    default: e = launch<32>(bwd, interleaved, n, a, s); break;
   }
   count_launch();
   return e;
@@ -411,17 +463,21 @@ cudaError_t launch(bool bwd, bool interleaved, const Args& a, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_headnorm_fwd(const Heads& h, cudaStream_t s) { return launch(false, h.interleaved, args_of(h), s); }
+cudaError_t launch_headnorm_fwd(const Heads& h, cudaStream_t s) {
+  const int n = heads_of_lane(h.heads_q, h.heads_k, h.dim);
+  return launch(false, h.interleaved, n, args_of(h, n), s);
+}
 
 int64_t headnorm_bwd_workspace_floats(int64_t rows, int heads_q, int heads_k, int dim) {
-  return (int64_t)ctas_of(rows * steps_of_row(heads_q, heads_k, dim), kBwdCtas) * 2 * dim;
+  return (int64_t)ctas_of(rows * steps_of_row(heads_q, heads_k, dim, heads_of_lane(heads_q, heads_k, dim)), kBwdCtas) * 2 * dim;
 }
 
 cudaError_t launch_headnorm_bwd(const Heads& h, cudaStream_t s) {
-  Args a = args_of(h);
+  const int n = heads_of_lane(h.heads_q, h.heads_k, h.dim);
+  Args a = args_of(h, n);
   const bool sums = h.dgain_q || h.dgain_k;
   a.partial = sums ? h.workspace : nullptr;
-  const cudaError_t e = launch(true, h.interleaved, a, s);
+  const cudaError_t e = launch(true, h.interleaved, n, a, s);
   if (e != cudaSuccess || !sums) return e;
   return launch_column_sums(h.workspace, ctas_of(a.steps, kBwdCtas), 2 * h.dim, h.dgain_q, h.accumulate, s, h.dgain_k, h.dim);
 }
