@@ -414,7 +414,8 @@ NVFP4_API nvfp4_status nvfp4_headnorm_bwd(const void* dy_bf16, int64_t lddy, con
  * nvfp4_embedding_fwd: out[i] = scale * table[token i] (n rows of cols).  A token outside of [0, vocab) (padding) gives a row of zeros.
  *   table: bf16 or binary32 (table_is_fp32) [vocab x cols], leading dimension ldt.  out: bf16 or binary32.
  * nvfp4_embedding_bwd: dtable[v] = (accumulate ? dtable[v] : 0) + scale * sum of dout[i] over the i whose token is v, added in binary32 in the
- *   order of i (in shares of that order where a token has many).  Padding adds nothing; with accumulate the rows of other tokens are not touched.
+ *   order of i (in shares of that order where a token has many).  Padding adds nothing; with accumulate the rows of other tokens are not touched, and
+ *   sums below 2^-126 count as 0.
  *   dout: bf16 or binary32 [n x cols].  dtable: binary32 [vocab x cols].
  *   workspace: nvfp4_embedding_bwd_workspace_bytes(n, vocab, cols).
  *   n, vocab up to 2^30.

@@ -1,11 +1,12 @@
 // Embedding lookup and the table's gradient.
 //   out[i] = scale table[token i];   dtable[v] (+)= scale sum of dout[i] over the i whose token is v
 // Both are bound by HBM: rows read, rows written.  For the gradient the tokens are sorted (stable, so that the order of a token's additions is that of
-// its places) and every sum is a run of the sorted list: no atomics, the same bits in every run.  Three launches:
-//   sort_kernel    a cluster of eight CTAs sorts (token, place) pairs by digits of up to nine bits; where the gradient is not added to what is
-//                  there, all other CTAs fill the table with zeros meanwhile
-//   runs_kernel    chunks of the sorted list: a run that lies in a chunk is written, one that crosses a border leaves partial sums
-//   joined_kernel  the runs that cross borders
+// its places) and every sum is a run of the sorted list: no order of additions that varies, the same bits in every run.
+//   sort_kernel    one CTA, or a cluster of eight, sorts (token, place) pairs by digits of up to nine bits
+//   zeros_kernel   where the gradient is not added to what is there, zeros in the whole table, beside the sort
+//   runs_kernel    chunks of the sorted list: whoever has the beginning of a run adds it up, over the end of its chunk too; of a run that has a whole
+//                  chunk in its middle every chunk leaves a partial sum
+//   joined_kernel  those long runs
 #include <algorithm>
 
 #include "around.h"
@@ -62,93 +63,94 @@ __device__ __forceinline__ Entry load_entry(const Entry* p) {
   return Entry{v.x, v.y};
 }
 
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kBins = 512;
+constexpr int kMaxSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kBins = 512, kSortTile = 4096;
 struct Sort {
   Indices tokens;
   Entry* sorted;
   Entry* other;
-  float* zero;  // NULL: the table's rows stay as they are
-  int64_t n, vocab, cols, ldt;
+  int64_t n, vocab;
   int passes, bits;  // digits of `bits` bits
 };
 struct SortShared {
   uint32_t counts[kSortWarps][kBins];
-  uint32_t total[kBins], base[kBins], of_warp[32];
+  uint32_t total[kBins], of_warp[32];
+  uint2 list[kSortTile];  // the CTA's part of the list, where it has room for it
 };
 
-// Zeros from shared memory, a piece at a time: one instruction stores 32 KB, so that a warp keeps an SM's stores going
-constexpr int kPiece = 32768;
-__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void fill_with_zeros(const Sort& a, uint8_t* smem) {
-  for (int i = threadIdx.x; i < kPiece / 16; i += kSortThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
-  fence_proxy_async_smem();
-  __syncthreads();
-  if (threadIdx.x >= 32) return;
-  const bool packed = a.ldt == a.cols;  // one long row then
-  const int64_t rows = packed ? 1 : a.vocab, bytes = (packed ? a.vocab : 1) * a.cols * 4, per_row = (bytes + kPiece - 1) / kPiece;
-  const int64_t stride = (int64_t)(gridDim.x - kSortCtas) * 32;
-  for (int64_t p = (int64_t)(blockIdx.x - kSortCtas) * 32 + threadIdx.x; p < rows * per_row; p += stride) {
-    const int64_t r = p / per_row, at = (p - r * per_row) * kPiece;
-    bulk_store(reinterpret_cast<uint8_t*>(a.zero + r * a.ldt) + at, smem_u32(smem), (uint32_t)min((int64_t)kPiece, bytes - at));
-  }
-  asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group 0;" ::: "memory");
-}
-
+// Every CTA, and in it every warp, has a part of the list.  A pass counts the digits of every warp's part, finds where each warp's first one of a digit
+// goes (behind all smaller digits, and behind the same one in the parts before), and moves the pairs.
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
   extern __shared__ __align__(16) uint8_t smem[];
   SortShared& sh = *reinterpret_cast<SortShared*>(smem);
   griddep_wait();
   griddep_launch_dependents();
-  if (blockIdx.x >= kSortCtas) {
-    fill_with_zeros(a, smem);
-    return;
-  }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x;
-  const int64_t c0 = a.n * rank / kSortCtas, c1 = a.n * (rank + 1) / kSortCtas;
-  const int64_t lo = c0 + (c1 - c0) * warp / kSortWarps, hi = c0 + (c1 - c0) * (warp + 1) / kSortWarps;
-  const uint32_t below = (1u << lane) - 1u, mask = (1u << a.bits) - 1u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x, ctas = gridDim.x, bins = 1 << a.bits;
+  const int64_t c0 = a.n * rank / ctas, c1 = a.n * (rank + 1) / ctas;
+  const int warps = (int)min((int64_t)kSortWarps, (c1 - c0 + 31) / 32);  // that have a part
+  const int64_t lo = warp < warps ? c0 + (c1 - c0) * warp / warps : c1, hi = warp < warps ? c0 + (c1 - c0) * (warp + 1) / warps : c1;
+  const uint32_t below = (1u << lane) - 1u, mask = bins - 1u;
+  const bool held = c1 - c0 <= kSortTile;
   for (int pass = 0; pass < a.passes; ++pass) {
     const bool even = (a.passes - 1 - pass) % 2 == 0;
     const Entry* const src = even ? a.other : a.sorted;
     Entry* const dst = even ? a.sorted : a.other;
     const int shift = pass * a.bits;
     auto entry = [&](int64_t i) {
-      if (pass > 0) return load_entry(src + i);
+      if (pass > 0) {
+        const Entry e = load_entry(src + i);
+        return make_uint2(e.token, e.place);
+      }
       const int64_t t = a.tokens[i];
-      return Entry{t >= 0 && t < a.vocab ? (uint32_t)t : (uint32_t)a.vocab, (uint32_t)i};
+      return make_uint2(t >= 0 && t < a.vocab ? (uint32_t)t : (uint32_t)a.vocab, (uint32_t)i);
     };
-    for (int b = threadIdx.x; b < kSortWarps * kBins; b += kSortThreads) (&sh.counts[0][0])[b] = 0u;
+    if (held)
+      for (int64_t i = c0 + threadIdx.x; i < c1; i += kSortThreads) sh.list[i - c0] = entry(i);
+    for (int b = threadIdx.x; b < warps * bins; b += kSortThreads) sh.counts[b >> a.bits][b & mask] = 0u;
     __syncthreads();
-    // how often each digit occurs in the warp's part of the list
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-      const bool live = i0 + lane < hi;
-      const uint32_t digit = live ? (entry(i0 + lane).token >> shift) & mask : ~0u;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    // four neighbouring groups of 32 whose loads are on their way together
+    auto each = [&](auto work) {
+      for (int64_t i0 = lo; i0 < hi; i0 += 128) {
+        uint2 e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int64_t i = i0 + 32 * u + lane;
+          e[u] = i < hi ? (held ? sh.list[i - c0] : entry(i)) : make_uint2(0u, 0u);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (i0 + 32 * u >= hi) break;
+          const bool live = i0 + 32 * u + lane < hi;
+          const uint32_t digit = live ? (e[u].x >> shift) & mask : ~0u;
+          work(e[u], digit, __match_any_sync(0xffffffffu, digit), live);
+          __syncwarp();
+        }
+      }
+    };
+    each([&](uint2, uint32_t digit, uint32_t same, bool live) {
       if (live && (same & below) == 0u) sh.counts[warp][digit] += __popc(same);
-      __syncwarp();
-    }
+    });
     __syncthreads();
-    // where its first one goes: behind all smaller digits, and behind the same one in the parts before
     uint32_t all = 0, before = 0;
-    if (threadIdx.x < kBins) {
+    if (threadIdx.x < bins) {
       uint32_t sum = 0;
 #pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) {
+      for (int w = 0; w < warps; ++w) {
         const uint32_t c = sh.counts[w][threadIdx.x];
         sh.counts[w][threadIdx.x] = sum;
         sum += c;
       }
-      sh.total[threadIdx.x] = sum;
+      sh.total[threadIdx.x] = all = sum;
     }
-    cluster_sync();
-    if (threadIdx.x < kBins) {
+    if (ctas > 1) {
+      cluster_sync();
+      if (threadIdx.x < bins) {
+        all = 0;
 #pragma unroll
-      for (int r = 0; r < kSortCtas; ++r) {
-        const uint32_t c = __float_as_uint(ld_of_rank(reinterpret_cast<const float*>(&sh.total[threadIdx.x]), r));
-        before += r < rank ? c : 0u;
-        all += c;
+        for (int r = 0; r < kMaxSortCtas; ++r) {
+          const uint32_t c = __float_as_uint(ld_of_rank(reinterpret_cast<const float*>(&sh.total[threadIdx.x]), r));
+          before += r < rank ? c : 0u;
+          all += c;
+        }
       }
     }
     uint32_t scan = all;
@@ -159,122 +161,178 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
     }
     if (lane == 31) sh.of_warp[warp] = scan;
     __syncthreads();
-    if (threadIdx.x < kBins) {
+    if (threadIdx.x < bins) {
       for (int w = 0; w < warp; ++w) scan += sh.of_warp[w];
       const uint32_t base = scan - all + before;
 #pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) sh.counts[w][threadIdx.x] += base;
+      for (int w = 0; w < warps; ++w) sh.counts[w][threadIdx.x] += base;
     }
     __syncthreads();
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-      const bool live = i0 + lane < hi;
-      Entry e{};
-      if (live) e = entry(i0 + lane);
-      const uint32_t digit = live ? (e.token >> shift) & mask : ~0u;
-      const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    each([&](uint2 e, uint32_t digit, uint32_t same, bool live) {
       uint32_t at = 0;
       if (live) at = sh.counts[warp][digit];
       __syncwarp();
       if (live) {
-        *reinterpret_cast<uint2*>(dst + at + __popc(same & below)) = make_uint2(e.token, e.place);
+        *reinterpret_cast<uint2*>(dst + at + __popc(same & below)) = e;
         if ((same & below) == 0u) sh.counts[warp][digit] = at + __popc(same);
       }
-      __syncwarp();
-    }
-    cluster_sync();  // the list is written, and nobody reads the totals any more
+    });
+    if (ctas > 1) cluster_sync(); else __syncthreads();  // the list is written, and nobody reads the totals any more
   }
 }
 
-constexpr int kRunThreads = 128, kBatch = 8;  // rows whose loads are on their way together
+// 32 KB of zeros to a CTA: CTAs that end and make room for the next ones keep to neighbouring memory, which HBM writes at 7.5 TB/s; resident ones that go
+// on with a stride drift apart (2.7 GB 360 us; 430 to 450 with strides, whether of stores or of bulk copies).  The launch before it is the sort, which has
+// waited for everything ahead of it and does not touch the table: the zeros need not wait for it, only the launch may not end before it.
+constexpr int kZeroThreads = 256, kZeros = 8 * kZeroThreads;  // of sixteen bytes
+__global__ void __launch_bounds__(kZeroThreads) zeros_kernel(float* table, int64_t rows, int64_t cols, int64_t ld) {
+  griddep_launch_dependents();
+  const int64_t c4 = cols >> 2, all = rows * c4, first = (int64_t)blockIdx.x * kZeros + threadIdx.x;
+  const bool packed = ld == cols;
+#pragma unroll
+  for (int k = 0; k < kZeros / kZeroThreads; ++k) {
+    const int64_t i = first + k * kZeroThreads;
+    if (i >= all) break;
+    const int64_t row = packed ? 0 : i / c4;
+    reinterpret_cast<float4*>(table + row * ld)[i - row * c4] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  if (blockIdx.x == gridDim.x - 1) griddep_wait();
+}
+
+constexpr int kRunThreads = 128, kRunRing = 8;  // rows that are on their way to a thread, and the one it works on
 struct Runs {
   const Entry* sorted;
   const void* dout;
   float* dtable;
-  float* head;  // per chunk: the sum of the run that reaches into it from the chunk before
-  float* tail;  // and of the run that begins in it and reaches into the next
-  int64_t n, vocab, cols, lddo, ldt, chunk, chunks;
-  int strips, threads;  // threads of a strip of columns; kRunThreads / threads chunks to a CTA
+  float* head;  // per chunk: of the long run that reaches into it from the chunk before
+  float* tail;  // and of the long run that begins in it
+  int64_t n, vocab, cols, lddo, ldt, chunks;
+  int chunk, strips, threads;  // threads of a strip of columns; kRunThreads / threads chunks to a CTA
   float scale;
   int accumulate;
 };
+// what a thread has of a row: sixteen bytes
+template <bool F32>
+constexpr int kWide = F32 ? 4 : 8;
 
-__device__ __forceinline__ void add_to_table(const Runs& a, uint32_t token, int64_t col, const float (&sum)[8]) {
+// Nobody else has these elements: an addition in memory instead of a load and a store leaves nothing to wait for (sums below 2^-126 come out as 0)
+__device__ __forceinline__ void add_four(float* p, float4 v) {
+  asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+template <int E>
+__device__ __forceinline__ void add_to_table(const Runs& a, uint32_t token, int64_t col, const float (&sum)[E]) {
   float* const p = a.dtable + (int64_t)token * a.ldt + col;
-  float v[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = sum[j] * a.scale;
-  if (a.accumulate) {
-    const float4 x = reinterpret_cast<const float4*>(p)[0], y = reinterpret_cast<const float4*>(p)[1];
-    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-    v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+  for (int j = 0; j < E; j += 4) {
+    const float4 v = make_float4(sum[j] * a.scale, sum[j + 1] * a.scale, sum[j + 2] * a.scale, sum[j + 3] * a.scale);
+    if (a.accumulate)
+      add_four(p + j, v);
+    else
+      *reinterpret_cast<float4*>(p + j) = v;
   }
-  store8<true>(p, 0, v);
 }
 
 template <bool F32>
 __global__ void __launch_bounds__(kRunThreads) runs_kernel(const Runs a) {
+  constexpr int E = kWide<F32>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  Entry* const list = reinterpret_cast<Entry*>(smem + kRunRing * kRunThreads * 16);
   griddep_wait();
   griddep_launch_dependents();
-  const int64_t group = blockIdx.x / a.strips, strip = blockIdx.x - group * a.strips;
-  const int64_t c = group * (kRunThreads / a.threads) + threadIdx.x / a.threads;
-  const int64_t col = (strip * a.threads + threadIdx.x % a.threads) * 8;
+  const int groups = kRunThreads / a.threads;
+  const int64_t group0 = blockIdx.x / a.strips * groups, strip = blockIdx.x % a.strips;
+  // the entries of the CTA's chunks, of the one before (and its predecessor) and of the one behind (and its successor)
+  const int64_t held0 = (group0 - 1) * a.chunk - 1;
+  for (int i = threadIdx.x; i < (groups + 2) * a.chunk + 2; i += kRunThreads) {
+    const int64_t at = held0 + i;
+    list[i] = at >= 0 && at < a.n ? load_entry(a.sorted + at) : Entry{~0u, 0u};  // (no token)
+  }
+  __syncthreads();
+  const int64_t c = group0 + threadIdx.x / a.threads, col = (strip * a.threads + threadIdx.x % a.threads) * E;
   if (c >= a.chunks || col >= a.cols) return;
-  const int64_t first = c * a.chunk, end = min(first + a.chunk, a.n);
-  const uint32_t before = first > 0 ? load_entry(a.sorted + first - 1).token : ~0u;
-  const uint32_t after = end < a.n ? load_entry(a.sorted + end).token : ~0u;
-  uint32_t token = load_entry(a.sorted + first).token;
-  bool from_before = token == before;
-  float sum[8] = {};
-  auto leave = [&](bool goes_on) {
-    if (token >= (uint32_t)a.vocab) return;
-    if (from_before)
-      store8<true>(a.head, c * a.cols + col, sum);
-    else if (goes_on)
-      store8<true>(a.tail, c * a.cols + col, sum);
-    else
-      add_to_table(a, token, col, sum);
+  const Entry* const mine = list + (threadIdx.x / a.threads + 1) * a.chunk + 1;  // the chunk's first; entries from -chunk - 1 to 2 chunk are there
+  const int size = (int)min((int64_t)a.chunk, a.n - c * a.chunk);
+  int i = 0, end = size;
+  bool from_before = mine[0].token == mine[-1].token;
+  if (from_before && mine[0].token != mine[-a.chunk - 1].token && mine[0].token != mine[size].token) {  // who has its beginning adds it up
+    while (i < size && mine[i].token == mine[0].token) ++i;
+    from_before = false;
+    if (i == size) return;
+  }
+  const uint32_t last = mine[size - 1].token;
+  const bool goes_on = mine[size].token == last && last < (uint32_t)a.vocab, of_end = mine[i].token == last && from_before;
+  const bool is_long = goes_on && (of_end || mine[size + a.chunk].token == last);
+  if (goes_on && !is_long)
+    while (mine[end].token == last) ++end;
+  const uint32_t ring = smem_u32(smem) + threadIdx.x * 16;
+  const uint8_t* const dout = static_cast<const uint8_t*>(a.dout) + col * (F32 ? 4 : 2);
+  const int64_t pitch = a.lddo * (F32 ? 4 : 2);
+  int ahead = i, slot = 0, next = 0;
+  auto fetch = [&] {
+    if (ahead < end && mine[ahead].token < (uint32_t)a.vocab) copy_async<16>(ring + next * (kRunThreads * 16), dout + mine[ahead].place * pitch, true);
+    copy_commit();  // (an empty group where there is no row: the count of groups stays that of the entries)
+    ++ahead;
+    next = next + 1 == kRunRing ? 0 : next + 1;
   };
-  for (int64_t i0 = first; i0 < end; i0 += kBatch) {
-    Entry e[kBatch];
-    Raw8<F32> raw[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) e[u] = i0 + u < end ? load_entry(a.sorted + i0 + u) : Entry{(uint32_t)a.vocab, 0u};
+  for (int u = 0; u < kRunRing - 1; ++u) fetch();
+  uint32_t token = mine[i].token;
+  float sum[E] = {};
+  for (; i < end; ++i) {
+    const uint32_t now = mine[i].token;
+    if (now >= (uint32_t)a.vocab) break;  // (padding stands at the end of the list)
+    if (now != token) {
+      if (from_before) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (e[u].token < (uint32_t)a.vocab)
-        raw[u].load(a.dout, (int64_t)e[u].place * a.lddo + col);
-      else
-        raw[u].zero();
-    }
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      if (i0 + u >= end) break;
-      if (e[u].token != token) {
-        leave(false);
-        token = e[u].token;
-        from_before = false;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+        for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(a.head + c * a.cols + col + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+      } else {
+        add_to_table(a, token, col, sum);
       }
-      float v[8];
-      raw[u].values(v);
+      token = now;
+      from_before = false;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += v[j];
+      for (int j = 0; j < E; ++j) sum[j] = 0.f;
+    }
+    copy_wait<kRunRing - 2>();
+    const uint4 raw = lds16(ring + slot * (kRunThreads * 16));
+    fetch();
+    slot = slot + 1 == kRunRing ? 0 : slot + 1;
+    if (F32) {
+      sum[0] += __uint_as_float(raw.x);
+      sum[1] += __uint_as_float(raw.y);
+      sum[2] += __uint_as_float(raw.z);
+      sum[3] += __uint_as_float(raw.w);
+    } else {
+      float2 v[4];
+      unpack8(raw, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sum[(2 * j) % E] += v[j].x;
+        sum[(2 * j + 1) % E] += v[j].y;
+      }
     }
   }
-  leave(token == after);
+  copy_wait<0>();
+  if (token >= (uint32_t)a.vocab) return;
+  float* const partial = from_before ? a.head : is_long ? a.tail : nullptr;
+  if (partial) {
+#pragma unroll
+    for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(partial + c * a.cols + col + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+  } else {
+    add_to_table(a, token, col, sum);
+  }
 }
 
-// A chunk whose last run begins in it and goes on: its tail and the heads of the chunks behind it that begin with the same token
+// A long run begins in the chunk: its tail and the heads of the chunks behind it that begin with the same token, in 64 bits
 __global__ void __launch_bounds__(kRunThreads) joined_kernel(const Runs a) {
   griddep_wait();
   griddep_launch_dependents();
   const int64_t c = blockIdx.x / a.strips, strip = blockIdx.x - c * a.strips;
   const int64_t first = c * a.chunk, next = first + a.chunk;
-  if (next >= a.n) return;
-  const uint32_t token = load_entry(a.sorted + next - 1).token;
-  if (token >= (uint32_t)a.vocab || load_entry(a.sorted + next).token != token) return;
-  if (first > 0 && load_entry(a.sorted + first - 1).token == token) return;  // (sorted: the whole chunk is this run then)
+  if (next + a.chunk >= a.n) return;
+  const uint32_t token = load_entry(a.sorted + next - 1).token, behind = load_entry(a.sorted + next + a.chunk).token;
+  const uint32_t before = first > 0 ? load_entry(a.sorted + first - 1).token : ~0u;
+  if (token != behind || token == before || token >= (uint32_t)a.vocab) return;
   const int lane = threadIdx.x & 31;
   int64_t more = 0;  // chunks that begin with the token
   while (true) {
@@ -284,28 +342,27 @@ __global__ void __launch_bounds__(kRunThreads) joined_kernel(const Runs a) {
     more += lead;
     if (lead < 32) break;
   }
-  const int64_t col = (strip * kRunThreads + threadIdx.x) * 8;
+  const int64_t col = (strip * kRunThreads + threadIdx.x) * 4;
   if (col >= a.cols) return;
-  const float4* const t = reinterpret_cast<const float4*>(a.tail + c * a.cols + col);
-  float4 x = t[0], y = t[1];
-  double s[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  float4 x = *reinterpret_cast<const float4*>(a.tail + c * a.cols + col);
+  double s[4] = {x.x, x.y, x.z, x.w};
   const float* h = a.head + (c + 1) * a.cols + col;
-#pragma unroll 4
+#pragma unroll 8
   for (int64_t k = 0; k < more; ++k, h += a.cols) {
-    const float4 u = reinterpret_cast<const float4*>(h)[0], v = reinterpret_cast<const float4*>(h)[1];
-    s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-    s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+    x = *reinterpret_cast<const float4*>(h);
+    s[0] += x.x;
+    s[1] += x.y;
+    s[2] += x.z;
+    s[3] += x.w;
   }
-  float sum[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sum[j] = (float)s[j];
+  const float sum[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
   add_to_table(a, token, col, sum);
 }
 
-// Entries of a chunk: few, so that few tokens fill the GPU, and at most some 1024 chunks, so that a run over all of them stays short
+// Entries of a chunk: few, so that few tokens fill the GPU, and more with their number, so that a run over all of them is of few partial sums
 int64_t chunk_of(int64_t n) {
   if (n <= 32768) return n <= 4096 ? 8 : n <= 8192 ? 16 : 32;
-  return ((n + 1023) / 1024 + 7) / 8 * 8;
+  return std::min<int64_t>(((n + 1023) / 1024 + 7) / 8 * 8, 256);
 }
 int64_t chunks_of(int64_t n) { return (n + chunk_of(n) - 1) / chunk_of(n); }
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -345,8 +402,7 @@ cudaError_t launch_embedding_bwd(const Embed& e, cudaStream_t s) {
   k.tokens = e.tokens;
   k.sorted = reinterpret_cast<Entry*>(take((size_t)e.n * sizeof(Entry)));
   k.other = reinterpret_cast<Entry*>(take((size_t)e.n * sizeof(Entry)));
-  k.zero = e.accumulate ? nullptr : static_cast<float*>(e.out);
-  k.n = e.n; k.vocab = e.vocab; k.cols = e.cols; k.ldt = e.ldt;
+  k.n = e.n; k.vocab = e.vocab;
   int bits = 1;
   while (((int64_t)1 << bits) <= e.vocab) ++bits;
   k.passes = (bits + 8) / 9;
@@ -355,24 +411,30 @@ cudaError_t launch_embedding_bwd(const Embed& e, cudaStream_t s) {
   int dev;
   cudaError_t err;
   if (device_needs_config(configured, &dev)) {
-    if ((err = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared))) != cudaSuccess)
+    if ((err = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared))) != cudaSuccess ||
+        (err = cudaFuncSetAttribute(runs_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024)) != cudaSuccess ||
+        (err = cudaFuncSetAttribute(runs_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024)) != cudaSuccess)
       return err;
     device_configured(configured, dev);
   }
-  unsigned grid = kSortCtas;
-  if (!e.accumulate) {  // a CTA for every 64 KB of zeros, two to an SM at most
-    const int64_t want = (e.vocab * e.cols * 4 + 65535) / 65536;
-    grid += (unsigned)((std::min<int64_t>(want, 2 * 148 - kSortCtas) + 7) / 8 * 8);
-  }
-  err = launch_cluster(kSortCtas, sort_kernel, dim3(grid), dim3(kSortThreads), sizeof(SortShared), s, k);
+  if (e.n <= kSortTile)
+    err = launch_divided(100, sort_kernel, dim3(1), dim3(kSortThreads), sizeof(SortShared), s, k);
+  else
+    err = launch_cluster(kMaxSortCtas, sort_kernel, dim3(kMaxSortCtas), dim3(kSortThreads), sizeof(SortShared), s, k);
   count_launch();
   if (err != cudaSuccess) return err;
+  if (!e.accumulate) {
+    err = launch_divided(-1, zeros_kernel, dim3((unsigned)((e.vocab * (e.cols / 4) + kZeros - 1) / kZeros)), dim3(kZeroThreads), 0, s,
+                         static_cast<float*>(e.out), e.vocab, e.cols, e.ldt);
+    count_launch();
+    if (err != cudaSuccess) return err;
+  }
 
   Runs r{};
   r.sorted = k.sorted;
   r.dout = e.table;
   r.dtable = static_cast<float*>(e.out);
-  r.chunk = chunk_of(e.n);
+  r.chunk = (int)chunk_of(e.n);
   r.chunks = chunks_of(e.n);
   r.head = reinterpret_cast<float*>(take((size_t)r.chunks * e.cols * 4));
   r.tail = reinterpret_cast<float*>(take((size_t)r.chunks * e.cols * 4));
@@ -380,15 +442,17 @@ cudaError_t launch_embedding_bwd(const Embed& e, cudaStream_t s) {
   r.lddo = e.ldo; r.ldt = e.ldt;
   r.scale = e.scale;
   r.accumulate = e.accumulate;
+  const int64_t wide = e.cols / (e.in_fp32 ? 4 : 8);
   r.threads = kRunThreads;
-  while (r.threads > 8 && r.threads / 2 >= e.cols / 8) r.threads /= 2;
-  r.strips = (int)((e.cols / 8 + r.threads - 1) / r.threads);
-  const int per_cta = kRunThreads / r.threads;
-  const int64_t ctas = (r.chunks + per_cta - 1) / per_cta * r.strips;
-  err = launch_divided(kStreamingCarveout, e.in_fp32 ? runs_kernel<true> : runs_kernel<false>, dim3((unsigned)ctas), dim3(kRunThreads), 0, s, r);
+  while (r.threads > 8 && r.threads / 2 >= wide) r.threads /= 2;
+  r.strips = (int)((wide + r.threads - 1) / r.threads);
+  const int groups = kRunThreads / r.threads;
+  const size_t smem = kRunRing * kRunThreads * 16 + ((size_t)(groups + 2) * r.chunk + 2) * sizeof(Entry);
+  err = launch_divided(100, e.in_fp32 ? runs_kernel<true> : runs_kernel<false>, dim3((unsigned)((r.chunks + groups - 1) / groups * r.strips)),
+                       dim3(kRunThreads), smem, s, r);
   count_launch();
-  if (err != cudaSuccess || r.chunks == 1) return err;
-  r.strips = (int)((e.cols / 8 + kRunThreads - 1) / kRunThreads);
+  if (err != cudaSuccess || r.chunks <= 2) return err;
+  r.strips = (int)((e.cols / 4 + kRunThreads - 1) / kRunThreads);
   err = launch_divided(kStreamingCarveout, joined_kernel, dim3((unsigned)(r.chunks * r.strips)), dim3(kRunThreads), 0, s, r);
   count_launch();
   return err;

@@ -360,7 +360,7 @@ struct Bwd {
   int64_t rows, vocab, ld, lddl, dcols, steps, per_row;
   float scale;
 };
-constexpr int kBwdCtas = 148 * 4;  // as many as are resident
+constexpr int kBwdCtas = 148 * 4, kBwdSteps = 32;  // as many as are resident; steps of a warp where there are more
 
 // Four or eight neighbours
 template <bool OUT32, int P>
@@ -395,7 +395,9 @@ struct RowGrad {
   }
 };
 
-// Every warp takes an equal share of all rows' steps of 32 chunks; the logits come through a ring as in the forward pass, and a row's
+// Every warp takes an equal share of all rows' steps of 32 chunks, 32 steps (16 KB) where there are enough for all: CTAs that end and make room for the
+// next ones keep to neighbouring memory, resident ones that go through long shares drift apart (8192 x 131072: 592 CTAs 760 us, 9472 640 us; 1003
+// x 50257 in binary32 with 592 / 1184 / 2368 / 9472 69 / 69 / 66 / 86); the logits come through a ring as in the forward pass, and a row's
 // numbers while the one before is worked on.
 template <bool F32, bool OUT32, bool ENTROPY>
 __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const Bwd a) {
@@ -511,7 +513,7 @@ cudaError_t launch_fwd(const Fwd& a, cudaStream_t s) {
 }
 template <bool F32, bool OUT32>
 cudaError_t launch_bwd(const Bwd& a, cudaStream_t s) {
-  const unsigned ctas = (unsigned)std::min<int64_t>((a.steps + kWarps - 1) / kWarps, kBwdCtas);
+  const unsigned ctas = (unsigned)std::max<int64_t>(a.steps / (kWarps * kBwdSteps), std::min<int64_t>((a.steps + kWarps - 1) / kWarps, kBwdCtas));
   const auto kern = a.dentropy ? logprob_bwd_kernel<F32, OUT32, true> : logprob_bwd_kernel<F32, OUT32, false>;
   return launch_divided(100, kern, dim3(ctas), dim3(kThreads), kRing * kStage, s, a);
 }
