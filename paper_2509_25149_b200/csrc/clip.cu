@@ -14,7 +14,8 @@ namespace nvfp4 {
 
 namespace {
 
-constexpr int kThreads = 256, kMaxCtas = 148 * 8, kAhead = 4, kTile = kThreads * kAhead * 8;  // elements of a tile: four chunks of eight a thread
+constexpr int kThreads = 256, kMaxCtas = 148 * 8, kAhead = 4;
+constexpr int kTile = kThreads * kAhead * 8, kSmallTile = kThreads * 8;  // elements of a tile: four chunks of eight a thread, or one where few tiles are too few for the GPU
 constexpr int kList = 600, kShortList = 64;  // tensors of a launch: 32 bytes each and 4 for the tiles before them, of 32764 bytes of parameters
 
 struct Tensor {
@@ -27,8 +28,8 @@ struct Tensor {
 template <int N>
 struct List {
   static constexpr int kMost = N;
-  int32_t n, tiles;
-  int32_t first[N];  // tiles before the tensor
+  int32_t n, tiles, tile;  // tile: elements
+  int32_t first[N];        // tiles before the tensor
   Tensor t[N];
 };
 
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(kThreads) sq_norm_kernel(const __grid_constant
   for (int tile = blockIdx.x; tile < l.tiles; tile += gridDim.x) {
     const int at = find(l, tile), k = tile - l.first[at];
     const Tensor& t = l.t[at];
-    const int64_t first = t.head + (int64_t)k * kTile, end = min(first + kTile, t.count);
+    const int64_t first = t.head + (int64_t)k * l.tile, end = min(first + l.tile, t.count);
     if (k == 0 && threadIdx.x < t.head) sum += square(element(t, threadIdx.x));
     sum += t.fp32 ? tile_squares<true>(t, first, end) : tile_squares<false>(t, first, end);
   }
@@ -131,8 +132,14 @@ __device__ __forceinline__ void scale_tile(const Tensor& t, int64_t first, int64
       static_cast<__nv_bfloat16*>(t.out)[i] = __float2bfloat16_rn(v);
   };
   if (!t.vector) {  // neighbouring threads take neighbouring elements
-#pragma unroll 8
-    for (int64_t i = first + threadIdx.x; i < end; i += kThreads) put(i, scaled(element(t, i)));
+    for (int64_t i = first + threadIdx.x; i < end; i += 8 * kThreads) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = i + j * kThreads < end ? element(t, i + j * kThreads) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i + j * kThreads < end) put(i + j * kThreads, scaled(v[j]));
+    }
     return;
   }
   Raw8<F32> raw[kAhead];
@@ -171,7 +178,7 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
     const int at = find(l, tile), k = tile - l.first[at];
     const Tensor& t = l.t[at];
     if (t.out == t.data && factor == 1.f) continue;
-    const int64_t first = t.head + (int64_t)k * kTile, end = min(first + kTile, t.count), from = k == 0 ? 0 : first;
+    const int64_t first = t.head + (int64_t)k * l.tile, end = min(first + l.tile, t.count), from = k == 0 ? 0 : first;
     if (from < first) {  // (at most seven)
       if (threadIdx.x < first) {
         const float v = factor == 0.f ? 0.f : element(t, threadIdx.x) * factor;
@@ -192,6 +199,9 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
 // The next tensors of a list, as many as a launch holds; returns how many of the list's it took
 template <class L>
 int fill(L& l, const nvfp4_grad* grads, int n) {
+  int64_t all = 0;
+  for (int i = 0; i < n; ++i) all += grads[i].count;
+  l.tile = all < (int64_t)kMaxCtas * kTile ? kSmallTile : kTile;
   l.n = 0;
   int64_t tiles = 0;
   int i = 0;
@@ -200,7 +210,7 @@ int fill(L& l, const nvfp4_grad* grads, int n) {
     if (g.count == 0) continue;
     const uintptr_t size = g.is_fp32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(g.data);
     const int64_t head = std::min<int64_t>((int64_t)((16 - at % 16) % 16 / size), g.count);
-    const int64_t of_tensor = std::max<int64_t>((g.count - head + kTile - 1) / kTile, 1);
+    const int64_t of_tensor = std::max<int64_t>((g.count - head + l.tile - 1) / l.tile, 1);
     if (tiles + of_tensor > INT_MAX) break;
     Tensor& t = l.t[l.n];
     t.data = g.data;

@@ -123,7 +123,8 @@ struct TopShared {
   uint64_t best[32];  // the group's likeliest, in order
   uint32_t top_of_thread[32 * W];
   uint64_t least;
-  int count;
+  int count, asked;
+  uint16_t asks[32 * W];  // threads whose elements are read again
 };
 
 // The likeliest of a group's share of a row.  Among the threads' maxima the top-th largest is no larger than the top-th largest element, so
@@ -132,10 +133,10 @@ struct TopShared {
 template <bool F32, int W>
 __device__ void select_top(const Fwd& a, TopShared<W>& sh, const void* row, float m, int64_t c0, int64_t c1, int64_t whole, int want) {
   constexpr int E = Chunk<F32>::E, T = 32 * W, kCandidates = TopShared<W>::kCandidates;
-  const int tid = threadIdx.x % T, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x % T, lane = tid & 31;
   sh.top_of_thread[tid] = ordered(m);
   group_sync<W>();
-  if (warp == 0) {
+  if (tid < 32) {
     uint32_t k[W], bound = 0;
 #pragma unroll
     for (int i = 0; i < W; ++i) k[i] = sh.top_of_thread[32 * i + lane];
@@ -148,14 +149,21 @@ __device__ void select_top(const Fwd& a, TopShared<W>& sh, const void* row, floa
     }
     if (lane == 0) sh.least = bound <= ordered(minus_infinity()) ? 0ull : (uint64_t)bound << 32;
   }
+  const int per = (int)((c1 - c0 + T - 1) / T);  // chunks of a thread, but for some threads' last one
   while (true) {
-    if (tid == 0) sh.count = 0;
+    if (tid == 0) sh.count = sh.asked = 0;
     group_sync<W>();
     const uint64_t least = sh.least;
-    const bool offers = ordered(m) >= (uint32_t)(least >> 32);
-    uint32_t asked = __ballot_sync(0xffffffffu, offers);
+    if (ordered(m) >= (uint32_t)(least >> 32)) sh.asks[atomicAdd(&sh.asked, 1)] = (uint16_t)tid;
+    group_sync<W>();
+    // all threads read the chunks of those that are asked, the first ones first, until there are too many candidates
+    const int asked = sh.asked;
     const volatile int* const so_far = &sh.count;
-    auto offer = [&](int64_t c) {
+#pragma unroll 4
+    for (int64_t p = tid; p < (int64_t)asked * per && *so_far <= kCandidates; p += T) {
+      const int turn = (int)(p / asked);
+      const int64_t c = c0 + (int64_t)turn * T + sh.asks[p - (int64_t)turn * asked];
+      if (c >= c1) continue;
       float2 v[E / 2];
       if (c < whole) {
         Chunk<F32> r;
@@ -172,20 +180,13 @@ __device__ void select_top(const Fwd& a, TopShared<W>& sh, const void* row, floa
           if (at < kCandidates) sh.keys[at] = key;
         }
       }
-    };
-    if (__popc(asked) > 4) {  // every lane its own chunks
-      if (offers)
-#pragma unroll 4
-        for (int64_t c = c0 + tid; c < c1 && *so_far <= kCandidates; c += T) offer(c);
-    } else {  // the lanes one after the other, a chunk to every lane
-      for (; asked; asked &= asked - 1)
-        for (int64_t c = c0 + warp * 32 + __ffs(asked) - 1 + (int64_t)lane * T; c < c1; c += 32 * T) offer(c);
     }
     group_sync<W>();
     const int count = sh.count, held = min(count, kCandidates);
     for (int i = tid; i < held; i += T) {
       const uint64_t key = sh.keys[i];
       int larger = 0;
+#pragma unroll 8
       for (int j = 0; j < held; ++j) larger += sh.keys[j] > key;
       if (larger < want) sh.best[larger] = key;
     }
@@ -340,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
         for (int i = tid; i < all; i += T) {
           const uint64_t key = sh.keys[i];
           int larger = 0;
+#pragma unroll 8
           for (int j = 0; j < all; ++j) larger += sh.keys[j] > key;
           if (larger < a.top) put(larger, key);
         }
