@@ -432,11 +432,11 @@ NVFP4_API nvfp4_status nvfp4_embedding_bwd(const void* tokens, int32_t tokens_ar
 /*
  * Log probabilities of given tokens, from logits [rows x vocab], bf16 or binary32 (logits_are_fp32); vocab is any number from one on (the
  * leading dimension's rule stands).  A logit of minus infinity (a token that is ruled out) has probability 0; it counts as a finite input here.
- *   z = scale * logit (2^-100 <= scale <= 2^100: one over the temperature),  lse = ln sum e^z,  log p = z - lse.
+ *   z = scale * logit (2^-60 <= scale <= 2^27: one over the temperature),  lse = ln sum e^z,  log p = z - lse.
  * nvfp4_logprob_fwd: each output may be NULL, not all.
  *   logprob: binary32 [rows], log p of the row's target; 0 where the target is outside of [0, vocab) (padding).  Wants targets.
  *   lse, entropy: binary32 [rows]; entropy = - sum p log p.
- *   stats: binary32 [rows x 2], 8-byte aligned: the row's largest logit and ln sum e^(z - largest z), which nvfp4_logprob_bwd takes (lse alone
+ *   stats: binary32 [rows x 2], 8-byte aligned: the row's largest logit and the binary logarithm of the sum beside it, which nvfp4_logprob_bwd takes (lse alone
  *   would not hold the sum beside a large logit).
  *   top_ids (int32), top_logprobs (binary32): [rows x top], the `top` likeliest tokens, likeliest first, equal ones by index; 1 <= top <=
  *   NVFP4_TOP_MAX and <= vocab where either is wanted.

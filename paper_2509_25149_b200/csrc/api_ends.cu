@@ -49,7 +49,7 @@ nvfp4_status check_embed(const Embed& e) {
 
 nvfp4_status check_logits(const Logprob& l) {
   if (l.rows <= 0 || l.rows > kMost || l.vocab <= 0 || l.vocab > kMost) return NVFP4_ERR_SHAPE;
-  if (!(l.scale >= 0x1p-100f && l.scale <= 0x1p100f)) return NVFP4_ERR_ARG;
+  if (!(l.scale >= 0x1p-60f && l.scale <= 0x1p27f)) return NVFP4_ERR_ARG;
   nvfp4_status st;
   if ((st = check_matrix(l.logits, l.ld, l.vocab, l.fp32)) != NVFP4_OK) return st;
   if (!aligned(l.stats, 8) || !aligned(l.entropy, 4)) return NVFP4_ERR_ALIGN;

@@ -2,8 +2,12 @@
 //   z = scale logit;  lse = ln sum e^z;  log p = z - lse;  H = - sum p log p
 //   gradient by a logit  scale (dlogprob ((j == target) - p) - dentropy p (log p + H))
 // Bound by HBM: the forward pass reads a row once, with the running maximum and the sums of e^(z - m) and (z - m) e^(z - m) in registers; the
-// gradient reads it once more and writes.  Differences from the maximum are taken of the logits before they are scaled: a row of the type's
-// lowest values keeps its distribution, and minus infinity gives e^z = 0 whatever stands beside it.
+// gradient reads it once more and writes.  In a long run the GPU is at its power limit, at 1.5 GHz for 1.96, and what an element costs in instructions
+// tells: everything is in powers of two, z log2(e) = x per, and a difference is one fused multiply-add, d = x per - ref.
+//   ref is the binary32 number nearest to m per, and what the sums are relative to: no rounding of m per is in any difference
+//   (one that all elements have in common would be, times the distance of the logits from zero).
+//   Logits more than 400 powers of two below the largest are taken for that far: p is 0 there all the same, and minus infinity has a finite
+//   difference, so that p d is 0 too.  Rows whose largest logit is beyond 2^90, those of the type's lowest values, say, take differences of the logits as they are.
 #include <algorithm>
 
 #include "around.h"
@@ -17,7 +21,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
 constexpr int kRing = 5, kStage = kThreads * 32;  // what is on its way to a CTA: 32 bytes a thread and stage
 constexpr int kShortRow = 4096;                   // up to here a warp takes a row by itself
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kLowest = -3.402823466e38f, kFar = -300.f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kLowest = -3.402823466e38f, kFar = -300.f, kReach = 400.f;
 
 __device__ __forceinline__ float exp2_fast(float v) {
   float r;
@@ -48,43 +52,20 @@ struct Fwd {
   int top;
 };
 
-// What a lane holds of its elements: the largest logit m (minus infinity: none), and for d = (x - max(m, lowest)) scale in powers of two the sums of 2^d and d 2^d
-template <bool ENTROPY>
-struct Running {
-  float m;
-  float2 s, t;
-  __device__ __forceinline__ Running() : m(minus_infinity()), s(make_float2(0.f, 0.f)), t(make_float2(0.f, 0.f)) {}
-  __device__ __forceinline__ float base() const { return fmaxf(m, kLowest); }
-  // the sums as those of differences from a larger maximum
-  __device__ __forceinline__ void raise(float to, float per) {
-    const float d = (base() - to) * per, f = exp2_fast(d);
-    if (ENTROPY) t = mul2(fma2(both(fmaxf(d, kFar)), s, t), both(f));  // (f is 0 below)
-    s = mul2(s, both(f));
-  }
-  template <int N>
-  __device__ __forceinline__ void add(const float2 (&v)[N], float largest, float per) {
-    if (largest > m) {
-      raise(fmaxf(largest, kLowest), per);
-      m = largest;
-    }
-    const float b = base();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float2 d = mul2(sub2(v[i], both(b)), both(per));
-      const float2 e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
-      s = add2(s, e);
-      if (ENTROPY) t = fma2(e, make_float2(fmaxf(d.x, kFar), fmaxf(d.y, kFar)), t);
-    }
-  }
-};
-
-template <bool F32>
-__device__ __forceinline__ float logit_at(const void* logits, int64_t at) {
-  return F32 ? static_cast<const float*>(logits)[at] : bf16_lo(static_cast<const uint16_t*>(logits)[at]);
-}
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
   const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+// the larger ones, NaN where there is one
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_nan(uint32_t a, uint32_t b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+  return __float_as_uint(r);
 }
 // Sixteen bytes of a row: eight or four neighbouring logits
 template <bool F32>
@@ -104,6 +85,20 @@ struct Chunk {
       v[3] = make_float2(bf16_lo(w.w), bf16_hi(w.w));
     }
   }
+  // the same with every value no lower than `least`: a binary32 number, or twice a bf16 one
+  __device__ __forceinline__ Chunk above(uint32_t least) const {
+    Chunk r;
+    r.w = F32 ? make_uint4(max_nan(w.x, least), max_nan(w.y, least), max_nan(w.z, least), max_nan(w.w, least))
+              : make_uint4(max_nan_bf16x2(w.x, least), max_nan_bf16x2(w.y, least), max_nan_bf16x2(w.z, least), max_nan_bf16x2(w.w, least));
+    return r;
+  }
+  // `least` of a number: rounded down
+  __device__ __forceinline__ static uint32_t held(float v) {
+    const uint32_t b = __float_as_uint(v);
+    if (F32) return b;
+    const uint32_t down = (b & 0x80000000u ? b + 0xffffu : b) >> 16;
+    return down << 16 | down;
+  }
   __device__ __forceinline__ float largest() const {
     if (F32) return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     const uint32_t m = max_bf16x2(max_bf16x2(w.x, w.y), max_bf16x2(w.z, w.w));
@@ -111,6 +106,94 @@ struct Chunk {
   }
 };
 
+constexpr float kNear = 0x1p90f;
+
+// What a row's differences are taken from: its largest logit (of the elements so far), m, minus infinity where there is none
+struct Reference {
+  float from, ref;  // near: 0 and fl(m per);  far: max(m, lowest) and 0
+  bool near;
+  __device__ __forceinline__ Reference(float m, float per) {
+    near = fabsf(m) <= kNear;
+    from = near ? 0.f : fmaxf(m, kLowest);
+    ref = near ? m * per : 0.f;
+  }
+  // of a logit, in powers of two
+  __device__ __forceinline__ float distance(float x, float per) const { return near ? fmaf(x, per, -ref) : (x - from) * per; }
+  // of what another reference stands for
+  __device__ __forceinline__ float distance(const Reference& r, float per) const {
+    return near && r.near ? r.ref - ref : ((r.near ? r.ref / per : r.from) - (near ? ref / per : from)) * per;
+  }
+};
+
+// What a lane holds of its elements: the largest logit m, and the sums of 2^d and d 2^d
+template <bool F32, bool ENTROPY>
+struct Running {
+  float m;
+  float2 s, t;
+  Reference at;
+  uint32_t least;
+  __device__ __forceinline__ Running(float per) : m(minus_infinity()), s(make_float2(0.f, 0.f)), t(make_float2(0.f, 0.f)), at(m, per), least(0u) {}
+  // the sums as those of differences from a larger maximum
+  __device__ __forceinline__ void raise(float to, float per, float reach) {
+    const Reference r(to, per);
+    const float d = r.distance(at, per), f = exp2_fast(d);
+    if (ENTROPY) t = mul2(fma2(both(fmaxf(d, kFar)), s, t), both(f));  // (f is 0 below)
+    s = mul2(s, both(f));
+    m = to;
+    at = r;
+    if (ENTROPY) least = Chunk<F32>::held(to - reach);
+  }
+  // TOGETHER: all lanes of the warp are here, and have one maximum: some ten times in a row there is a larger one, where every lane's own would be
+  // exceeded in one lane or another nearly every time.  Returns the largest of these.
+  template <bool TOGETHER, int N>
+  __device__ __forceinline__ float add(const Chunk<F32> (&raw)[N], float per, float reach) {
+    constexpr int P = Chunk<F32>::kPairs;
+    float largest = raw[0].largest();
+#pragma unroll
+    for (int u = 1; u < N; ++u) largest = fmaxf(largest, raw[u].largest());
+    if (TOGETHER) {
+      if (__any_sync(0xffffffffu, largest > m)) raise(of_ordered(__reduce_max_sync(0xffffffffu, ordered(largest))), per, reach);
+    } else if (largest > m) {
+      raise(largest, per, reach);
+    }
+    if (__builtin_expect(at.near, 1)) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        float2 v[P];
+        (ENTROPY ? raw[u].above(least) : raw[u]).values(v);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const float2 d = fma2(v[i], both(per), both(-at.ref)), e = make_float2(exp2_fast(d.x), exp2_fast(d.y));
+          s = add2(s, e);
+          if (ENTROPY) t = fma2(e, d, t);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        float2 v[P];
+        raw[u].values(v);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          one(v[i].x, per);
+          one(v[i].y, per);
+        }
+      }
+    }
+    return largest;
+  }
+  // a single one, no larger than m
+  __device__ __forceinline__ void one(float x, float per) {
+    const float d = at.distance(x, per), e = exp2_fast(d);
+    s.x += e;
+    if (ENTROPY) t.x = fmaf(e, fmaxf(d, kFar), t.x);
+  }
+};
+
+template <bool F32>
+__device__ __forceinline__ float logit_at(const void* logits, int64_t at) {
+  return F32 ? static_cast<const float*>(logits)[at] : bf16_lo(static_cast<const uint16_t*>(logits)[at]);
+}
 // A row belongs to a group of W warps
 template <int W>
 __device__ __forceinline__ void group_sync() {
@@ -218,50 +301,54 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
   const uint8_t* const x = static_cast<const uint8_t*>(a.logits) + row * a.ld * (F32 ? 4 : 2);
   const int64_t whole = a.vocab / E, chunks = (a.vocab + E - 1) / E;
   const int64_t c0 = chunks * part / parts, c1 = chunks * (part + 1) / parts, full = min(c1, whole);
-  const float per = a.scale * kLog2e;
-  Running<ENTROPY> run;
+  const float per = a.scale * kLog2e, reach = kReach / per;
+  Running<F32, ENTROPY> run(per);
   // the row comes through a ring in which every thread has places of its own
   const uint32_t mine = smem_u32(smem) + threadIdx.x * 16;
-  int64_t ahead = c0 + tid;
-  auto fetch = [&](int slot) {
+  auto chunks_of = [&](int t) { return (int)max((full - c0 - t + T - 1) / T, (int64_t)0); };
+  const int n = chunks_of(tid), stages = chunks_of(tid | 31) / kChunks;  // the thread's chunks; stages that are full for all of its warp
+  float own = minus_infinity();  // (a NaN is nobody's maximum)
+  const uint8_t* from = x + (c0 + tid) * 16;
+  int asked = 0;
+  auto fetch = [&](uint32_t to) {
 #pragma unroll
-    for (int u = 0; u < kChunks; ++u, ahead += T)
-      if (ahead < full) copy_async<16>(mine + slot * kStage + u * (kThreads * 16), x + ahead * 16, true);
+    for (int u = 0; u < kChunks; ++u)
+      if (asked + u < n) copy_async<16>(to + u * (kThreads * 16), from + u * (T * 16), true);
+    asked += kChunks;
+    from += kChunks * T * 16;
     copy_commit();  // (an empty group where there is no chunk: the count of groups stays that of the stages)
   };
 #pragma unroll
-  for (int u = 0; u < kRing - 1; ++u) fetch(u);
-  int slot = 0, next = kRing - 1;
-  for (int64_t c = c0 + tid; c < full; c += T * kChunks) {
+  for (int u = 0; u < kRing - 1; ++u) fetch(mine + u * kStage);
+  uint32_t at = mine, before = mine + (kRing - 1) * kStage;
+  for (int i = 0; i < stages; ++i) {
     copy_wait<kRing - 2>();
     Chunk<F32> raw[kChunks];
 #pragma unroll
-    for (int u = 0; u < kChunks; ++u) {
-      raw[u].w = lds16(mine + slot * kStage + u * (kThreads * 16));
-      if (u > 0 && c + u * T >= full) raw[u].nothing();
-    }
-    fetch(next);  // the slot of the stage before, whose values went into registers a turn ago
-    slot = slot + 1 == kRing ? 0 : slot + 1;
-    next = next + 1 == kRing ? 0 : next + 1;
-    float2 v[kChunks * E / 2];
-    float largest = minus_infinity();
-#pragma unroll
-    for (int u = 0; u < kChunks; ++u) {
-      raw[u].values(v + u * (E / 2));
-      largest = fmaxf(largest, raw[u].largest());
-    }
-    run.add(v, largest, per);
+    for (int u = 0; u < kChunks; ++u) raw[u].w = lds16(at + u * (kThreads * 16));
+    fetch(before);  // the place of the stage before, whose values went into registers a turn ago
+    before = at;
+    at = at == mine + (kRing - 1) * kStage ? mine : at + kStage;
+    const float largest = run.template add<true>(raw, per, reach);
+    if (TOP) own = fmaxf(own, largest);
   }
   copy_wait<0>();
+  for (int i = stages * kChunks; i < n; ++i) {  // (two at most)
+    Chunk<F32> raw[1];
+    raw[0].w = lds16(at + (i % kChunks) * (kThreads * 16));
+    if (i % kChunks == kChunks - 1) at = at == mine + (kRing - 1) * kStage ? mine : at + kStage;
+    own = fmaxf(own, run.template add<false>(raw, per, reach));
+  }
   if (c1 > whole && tid == (int)((whole - c0) % T)) {  // a last chunk that is not full, to the thread whose turn it is
     for (int64_t j = whole * E; j < a.vocab; ++j) {
-      const float2 v[1] = {make_float2(logit_at<F32>(x, j), minus_infinity())};
-      run.add(v, v[0].x, per);
+      const float v = logit_at<F32>(x, j);
+      own = fmaxf(own, v);
+      if (v > run.m) run.raise(v, per, reach);
+      run.one(v, per);
     }
   }
-  const float own = run.m;
   // the group's maximum, then sums of differences from it
-  float m = own;
+  float m = run.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (W > 1) {
@@ -271,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
 #pragma unroll
     for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   }
-  run.raise(fmaxf(m, kLowest), per);
+  run.raise(m, per, reach);
   float s = run.s.x + run.s.y, t = run.t.x + run.t.y;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -305,28 +392,35 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
       if (parts > 1) {
         for (uint32_t r = 1; r < parts; ++r) m = fmaxf(m, ld_of_rank(&of_cta.m, r));
         s = t = 0.f;
+        const Reference whole_row(m, per);
         for (uint32_t r = 0; r < parts; ++r) {
-          const float d = (fmaxf(ld_of_rank(&of_cta.m, r), kLowest) - fmaxf(m, kLowest)) * per, f = exp2_fast(d), sr = ld_of_rank(&of_cta.s, r);
+          const float d = whole_row.distance(Reference(ld_of_rank(&of_cta.m, r), per), per), f = exp2_fast(d), sr = ld_of_rank(&of_cta.s, r);
           s += f * sr;
           if (ENTROPY) t += f * fmaf(fmaxf(d, kFar), sr, ld_of_rank(&of_cta.t, r));
         }
       }
     }
-    const float base = fmaxf(m, kLowest), log_total = logf(s);
+    const Reference ref(m, per);
+    const float log_total = log2f(s);
+    auto log_p = [&](float v) {
+      const float d = ref.distance(v, per);
+      if (s == 0.f) return minus_infinity();
+      // (far out, nothing beside the difference counts, which may fit binary32 while that many powers of two do not)
+      return d < -0x1p60f ? (v - fmaxf(m, kLowest)) * a.scale : kLn2 * (d - log_total);
+    };
     if (tid == 0) {
-      if (a.lse) a.lse[row] = fmaf(base, a.scale, log_total);
+      if (a.lse) a.lse[row] = fmaf(fmaxf(m, kLowest), a.scale, kLn2 * log_total);
       if (a.stats) a.stats[row] = make_float2(m, log_total);
-      if (a.entropy) a.entropy[row] = s == 0.f ? 0.f : log_total - kLn2 * (t / s);
+      if (a.entropy) a.entropy[row] = s == 0.f ? 0.f : kLn2 * (log_total - t / s);
       if (a.logprob) {
         const int64_t target = a.targets[row];
-        a.logprob[row] = target < 0 || target >= a.vocab ? 0.f : s == 0.f ? minus_infinity() : (logit_at<F32>(x, target) - base) * a.scale - log_total;
+        a.logprob[row] = target < 0 || target >= a.vocab ? 0.f : log_p(logit_at<F32>(x, target));
       }
     }
     if (TOP) {
       auto put = [&](int place, uint64_t key) {
         if (a.top_ids) a.top_ids[row * a.top + place] = (int)~(uint32_t)key;
-        if (a.top_logprobs)
-          a.top_logprobs[row * a.top + place] = s == 0.f ? minus_infinity() : (of_ordered((uint32_t)(key >> 32)) - base) * a.scale - log_total;
+        if (a.top_logprobs) a.top_logprobs[row * a.top + place] = log_p(of_ordered((uint32_t)(key >> 32)));
       };
       if (parts == 1) {
         if (tid < a.top) put(tid, sh.best[tid]);
@@ -378,22 +472,28 @@ __device__ __forceinline__ void put(void* out, int64_t at, const float2 (&v)[P])
   }
 }
 
-// What a row's gradient is made of: p = 2^(d per - total) with d = x - top, and the gradient p (a + b log2 p), with `hit` more at the target
+// What a row's gradient is made of: log2 p = d - total, d the distance from the row's reference, and the gradient p (a + b log2 p), with `hit` more at the target
 struct RowGrad {
-  float top, total, a, b, hit;
-  int64_t target;
-  template <bool ENTROPY>
+  Reference at;
+  float total, a, b, hit;
+  uint32_t least;
+  int target_chunk, target_place;  // -1: none
+  __device__ __forceinline__ RowGrad() : at(0.f, 0.f) {}
+  template <bool F32, bool ENTROPY>
   __device__ __forceinline__ void load(const Bwd& g, int64_t row) {
     const float2 st = g.stats[row];
     const int64_t t = g.targets.p ? g.targets[row] : -1;
     const float w = g.dlogprob ? g.dlogprob[row] * g.scale : 0.f, e = ENTROPY ? g.dentropy[row] * g.scale : 0.f, h = ENTROPY ? g.entropy[row] : 0.f;
     const bool empty = st.x == minus_infinity(), there = t >= 0 && t < g.vocab && !empty;
-    top = empty ? 0.f : st.x;  // (all of an empty row is p = 0 then)
-    total = empty ? 0.f : st.y * kLog2e;
+    const float m = empty ? 0.f : st.x, per = g.scale * kLog2e;  // (all of an empty row is p = 0 then)
+    at = Reference(m, per);
+    least = Chunk<F32>::held(m - kReach / per);
+    total = empty ? 0.f : st.y;
     hit = there ? w : 0.f;
     a = -fmaf(e, h, hit);
     b = -e * kLn2;
-    target = there ? t : -1;
+    target_chunk = there ? (int)(t / Chunk<F32>::E) : -1;
+    target_place = (int)(t % Chunk<F32>::E);
   }
 };
 
@@ -406,20 +506,26 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const Bwd a) {
   constexpr int E = Chunk<F32>::E, kSlots = kRing * 2, kSlot = kThreads * 16;
   extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31;
-  const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int64_t first = a.steps * w / warps, steps = a.steps * (w + 1) / warps - first, whole = a.vocab / E;
+  const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5), first = a.steps * w / warps;
+  const int steps = (int)(a.steps * (w + 1) / warps - first), whole = (int)(a.vocab / E), of_row = (int)a.per_row * 32;
   const uint32_t mine = smem_u32(smem) + threadIdx.x * 16;
-  int64_t row = first / a.per_row, c = (first - row * a.per_row) * 32 + lane;  // a lane's chunk
-  int64_t ahead_row = row, ahead = c, fetched = 0;
-  const uint8_t* const x = static_cast<const uint8_t*>(a.logits);
-  auto fetch = [&](int slot) {
-    if (fetched < steps) {
-      if (ahead < whole) copy_async<16>(mine + slot * kSlot, x + ahead_row * a.ld * (F32 ? 4 : 2) + ahead * 16, true);
-      ++fetched;
+  int64_t row = first / a.per_row;
+  int c = (int)(first - row * a.per_row) * 32 + lane;  // a lane's chunk
+  const int64_t pitch = a.ld * (F32 ? 4 : 2), out_pitch = a.lddl * (OUT32 ? 4 : 2);
+  const uint8_t* ahead_row = static_cast<const uint8_t*>(a.logits) + row * pitch;
+  uint8_t* out = static_cast<uint8_t*>(a.dlogits) + row * out_pitch + (int64_t)c * (E * (OUT32 ? 4 : 2));
+  int ahead = c, asked = 0;
+  const uint8_t* from = ahead_row + (int64_t)ahead * 16;
+  auto fetch = [&](uint32_t to) {
+    if (asked < steps) {
+      if (ahead < whole) copy_async<16>(to, from, true);
+      ++asked;
       ahead += 32;
-      if (ahead >= a.per_row * 32) {
+      from += 512;
+      if (ahead >= of_row) {
         ahead = lane;
-        ++ahead_row;
+        ahead_row += pitch;
+        from = ahead_row + lane * 16;
       }
     }
     copy_commit();
@@ -428,55 +534,67 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const Bwd a) {
   griddep_launch_dependents();
   if (steps == 0) return;
 #pragma unroll
-  for (int u = 0; u < kSlots - 1; ++u) fetch(u);
-  int slot = 0, next = kSlots - 1;
+  for (int u = 0; u < kSlots - 1; ++u) fetch(mine + u * kSlot);
+  uint32_t at = mine, before = mine + (kSlots - 1) * kSlot;
   RowGrad now, then;
-  now.load<ENTROPY>(a, row);
+  now.load<F32, ENTROPY>(a, row);
   then = now;
-  if (row + 1 < a.rows) then.load<ENTROPY>(a, row + 1);
+  if (row + 1 < a.rows) then.load<F32, ENTROPY>(a, row + 1);
   const float per = a.scale * kLog2e;
-  auto grad = [&](float2 v) {
-    const float2 l = fma2(sub2(v, both(now.top)), both(per), both(-now.total)), p = make_float2(exp2_fast(l.x), exp2_fast(l.y));
-    if (!ENTROPY) return mul2(p, both(now.a));
-    return mul2(p, fma2(make_float2(fmaxf(l.x, kFar), fmaxf(l.y, kFar)), both(now.b), both(now.a)));  // (p is 0 below)
+  auto distance = [&](float v) { return __uint_as_float(max_nan(__float_as_uint(now.at.distance(v, per)), __float_as_uint(-kReach))); };
+  auto grad = [&](float2 v) {  // of distances
+    const float2 l = add2(v, both(-now.total)), p = make_float2(exp2_fast(l.x), exp2_fast(l.y));
+    return mul2(p, ENTROPY ? fma2(l, both(now.b), both(now.a)) : both(now.a));
   };
-  for (int64_t i = 0; i < steps; ++i) {
+  for (int i = 0; i < steps; ++i) {
     copy_wait<kSlots - 2>();
     if (c < whole) {
       Chunk<F32> raw;
-      raw.w = lds16(mine + slot * kSlot);
+      raw.w = lds16(at);
       float2 v[E / 2];
-      raw.values(v);
+      if (__builtin_expect(now.at.near, 1)) {
+        (ENTROPY ? raw.above(now.least) : raw).values(v);
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) v[j] = fma2(v[j], both(per), both(-now.at.ref));
+      } else {
+        raw.values(v);
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) v[j] = make_float2(distance(v[j].x), distance(v[j].y));
+      }
 #pragma unroll
       for (int j = 0; j < E / 2; ++j) v[j] = grad(v[j]);
-      if (c == now.target / E && now.target >= 0) {
-        const int at = (int)(now.target % E);
+      if (c == now.target_chunk) {
 #pragma unroll
         for (int j = 0; j < E / 2; ++j) {
-          if (at == 2 * j) v[j].x += now.hit;
-          if (at == 2 * j + 1) v[j].y += now.hit;
+          if (now.target_place == 2 * j) v[j].x += now.hit;
+          if (now.target_place == 2 * j + 1) v[j].y += now.hit;
         }
       }
-      put<OUT32>(a.dlogits, row * a.lddl + c * E, v);
+      put<OUT32>(out, 0, v);
     } else {  // what is left of the columns, and zeros behind them
-      for (int64_t j = c * E; j < min(c * E + E, a.dcols); ++j) {
+      const int left = (int)min((int64_t)E, a.dcols - (int64_t)c * E), held = (int)min((int64_t)E, a.vocab - (int64_t)c * E);
+      for (int j = 0; j < left; ++j) {
         float g = 0.f;
-        if (j < a.vocab) g = grad(both(logit_at<F32>(x, row * a.ld + j))).x + (j == now.target ? now.hit : 0.f);
+        if (j < held)
+          g = grad(both(distance(logit_at<F32>(static_cast<const uint8_t*>(a.logits) + row * pitch, (int64_t)c * E + j)))).x +
+              (c == now.target_chunk && j == now.target_place ? now.hit : 0.f);
         if (OUT32)
-          static_cast<float*>(a.dlogits)[row * a.lddl + j] = g;
+          reinterpret_cast<float*>(out)[j] = g;
         else
-          static_cast<__nv_bfloat16*>(a.dlogits)[row * a.lddl + j] = __float2bfloat16_rn(g);
+          reinterpret_cast<__nv_bfloat16*>(out)[j] = __float2bfloat16_rn(g);
       }
     }
-    fetch(next);
-    slot = slot + 1 == kSlots ? 0 : slot + 1;
-    next = next + 1 == kSlots ? 0 : next + 1;
+    fetch(before);
+    before = at;
+    at = at == mine + (kSlots - 1) * kSlot ? mine : at + kSlot;
     c += 32;
-    if (c >= a.per_row * 32) {
+    out += 32 * E * (OUT32 ? 4 : 2);
+    if (c >= of_row) {
       c = lane;
       ++row;
+      out = static_cast<uint8_t*>(a.dlogits) + row * out_pitch + lane * (E * (OUT32 ? 4 : 2));
       now = then;
-      if (i + 1 < steps && row + 1 < a.rows) then.load<ENTROPY>(a, row + 1);
+      if (i + 1 < steps && row + 1 < a.rows) then.load<F32, ENTROPY>(a, row + 1);
     }
   }
   copy_wait<0>();
