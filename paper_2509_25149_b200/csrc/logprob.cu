@@ -389,15 +389,23 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
       m = of_cta.m;
       s = of_cta.s;
       t = of_cta.t;
-      if (parts > 1) {
-        for (uint32_t r = 1; r < parts; ++r) m = fmaxf(m, ld_of_rank(&of_cta.m, r));
-        s = t = 0.f;
-        const Reference whole_row(m, per);
-        for (uint32_t r = 0; r < parts; ++r) {
-          const float d = whole_row.distance(Reference(ld_of_rank(&of_cta.m, r), per), per), f = exp2_fast(d), sr = ld_of_rank(&of_cta.s, r);
-          s += f * sr;
-          if (ENTROPY) t += f * fmaf(fmaxf(d, kFar), sr, ld_of_rank(&of_cta.t, r));
+      if (parts > 1) {  // a lane to a CTA
+        const uint32_t r = lane < (int)parts ? lane : 0;
+        const float mr = ld_of_rank(&of_cta.m, r), sr = ld_of_rank(&of_cta.s, r), tr = ENTROPY ? ld_of_rank(&of_cta.t, r) : 0.f;
+        m = mr;
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        m = __shfl_sync(0xffffffffu, m, 0);
+        const float d = Reference(m, per).distance(Reference(mr, per), per), f = lane < (int)parts ? exp2_fast(d) : 0.f;
+        s = f * sr;
+        t = f * fmaf(fmaxf(d, kFar), sr, tr);
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+          s += __shfl_xor_sync(0xffffffffu, s, o);
+          if (ENTROPY) t += __shfl_xor_sync(0xffffffffu, t, o);
         }
+        s = __shfl_sync(0xffffffffu, s, 0);
+        if (ENTROPY) t = __shfl_sync(0xffffffffu, t, 0);
       }
     }
     const Reference ref(m, per);
