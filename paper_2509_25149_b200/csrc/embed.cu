@@ -2,7 +2,8 @@
 //   out[i] = scale table[token i];   dtable[v] (+)= scale sum of dout[i] over the i whose token is v
 // Both are bound by HBM: rows read, rows written.  For the gradient the tokens are sorted (stable, so that the order of a token's additions is that of
 // its places) and every sum is a run of the sorted list: no order of additions that varies, the same bits in every run.
-//   sort_kernel    one CTA, or a cluster of eight, sorts (token, place) pairs by digits of up to nine bits
+//   rank_kernel    few tokens: a warp counts how many stand before its token
+//   sort_kernel    more: a cluster of eight CTAs sorts (token, place) pairs by digits of up to nine bits
 //   zeros_kernel   where the gradient is not added to what is there, zeros in the whole table, beside the sort
 //   runs_kernel    chunks of the sorted list: whoever has the beginning of a run adds it up, over the end of its chunk too; of a run that has a whole
 //                  chunk in its middle every chunk leaves a partial sum
@@ -63,7 +64,7 @@ __device__ __forceinline__ Entry load_entry(const Entry* p) {
   return Entry{v.x, v.y};
 }
 
-constexpr int kMaxSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kBins = 512, kSortTile = 4096;
+constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kBins = 512, kSortTile = 4096;
 struct Sort {
   Indices tokens;
   Entry* sorted;
@@ -77,6 +78,29 @@ struct SortShared {
   uint2 list[kSortTile];  // the CTA's part of the list, where it has room for it
 };
 
+// A token's place in the sorted list is the number of smaller ones and of equal ones before it.  That is n^2 / 32 steps for n tokens, without a barrier or
+// a round trip to memory beside the first (1003 tokens 11.4 us in the sort by one CTA, 4 here); from some thousands on the sort is the shorter way.
+constexpr int kRankThreads = 256, kRankMost = 4096;
+__global__ void __launch_bounds__(kRankThreads) rank_kernel(const Sort a) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int i = blockIdx.x * (kRankThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31, n = (int)a.n;
+  if (i >= n) return;
+  auto token = [&](int j) {
+    const int64_t t = a.tokens[j];
+    return t >= 0 && t < a.vocab ? (uint32_t)t : (uint32_t)a.vocab;
+  };
+  const uint32_t mine = token(i);
+  int before = 0;
+#pragma unroll 8
+  for (int j = lane; j < n; j += 32) {
+    const uint32_t t = token(j);
+    before += t < mine || (t == mine && j < i);
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0) *reinterpret_cast<uint2*>(a.sorted + before) = make_uint2(mine, (uint32_t)i);
+}
+
 // Every CTA, and in it every warp, has a part of the list.  A pass counts the digits of every warp's part, finds where each warp's first one of a digit
 // goes (behind all smaller digits, and behind the same one in the parts before), and moves the pairs.
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
@@ -84,8 +108,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
   SortShared& sh = *reinterpret_cast<SortShared*>(smem);
   griddep_wait();
   griddep_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x, ctas = gridDim.x, bins = 1 << a.bits;
-  const int64_t c0 = a.n * rank / ctas, c1 = a.n * (rank + 1) / ctas;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x, bins = 1 << a.bits;
+  const int64_t c0 = a.n * rank / kSortCtas, c1 = a.n * (rank + 1) / kSortCtas;
   const int warps = (int)min((int64_t)kSortWarps, (c1 - c0 + 31) / 32);  // that have a part
   const int64_t lo = warp < warps ? c0 + (c1 - c0) * warp / warps : c1, hi = warp < warps ? c0 + (c1 - c0) * (warp + 1) / warps : c1;
   const uint32_t below = (1u << lane) - 1u, mask = bins - 1u;
@@ -139,18 +163,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
         sh.counts[w][threadIdx.x] = sum;
         sum += c;
       }
-      sh.total[threadIdx.x] = all = sum;
+      sh.total[threadIdx.x] = sum;
     }
-    if (ctas > 1) {
-      cluster_sync();
-      if (threadIdx.x < bins) {
-        all = 0;
+    cluster_sync();
+    if (threadIdx.x < bins) {
+      all = 0;
 #pragma unroll
-        for (int r = 0; r < kMaxSortCtas; ++r) {
-          const uint32_t c = __float_as_uint(ld_of_rank(reinterpret_cast<const float*>(&sh.total[threadIdx.x]), r));
-          before += r < rank ? c : 0u;
-          all += c;
-        }
+      for (int r = 0; r < kSortCtas; ++r) {
+        const uint32_t c = __float_as_uint(ld_of_rank(reinterpret_cast<const float*>(&sh.total[threadIdx.x]), r));
+        before += r < rank ? c : 0u;
+        all += c;
       }
     }
     uint32_t scan = all;
@@ -177,7 +199,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
         if ((same & below) == 0u) sh.counts[warp][digit] = at + __popc(same);
       }
     });
-    if (ctas > 1) cluster_sync(); else __syncthreads();  // the list is written, and nobody reads the totals any more
+    cluster_sync();  // the list is written, and nobody reads the totals any more
   }
 }
 
@@ -417,10 +439,10 @@ cudaError_t launch_embedding_bwd(const Embed& e, cudaStream_t s) {
       return err;
     device_configured(configured, dev);
   }
-  if (e.n <= kSortTile)
-    err = launch_divided(100, sort_kernel, dim3(1), dim3(kSortThreads), sizeof(SortShared), s, k);
+  if (e.n <= kRankMost)
+    err = launch_divided(-1, rank_kernel, dim3((unsigned)((e.n + kRankThreads / 32 - 1) / (kRankThreads / 32))), dim3(kRankThreads), 0, s, k);
   else
-    err = launch_cluster(kMaxSortCtas, sort_kernel, dim3(kMaxSortCtas), dim3(kSortThreads), sizeof(SortShared), s, k);
+    err = launch_cluster(kSortCtas, sort_kernel, dim3(kSortCtas), dim3(kSortThreads), sizeof(SortShared), s, k);
   count_launch();
   if (err != cudaSuccess) return err;
   if (!e.accumulate) {
