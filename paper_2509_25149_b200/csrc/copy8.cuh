@@ -224,6 +224,17 @@ __device__ __forceinline__ void store8(void* base, int64_t elem, const float (&v
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + elem) = pack8(v);
   }
 }
+// the same for results that exceed L2 and are not read again by their kernel: first to leave it, so that what is read stays
+template <bool F32>
+__device__ __forceinline__ void store8_first_out(void* base, int64_t elem, const float (&v)[8]) {
+  if (F32) {
+    float4* p = reinterpret_cast<float4*>(static_cast<float*>(base) + elem);
+    __stcs(p, make_float4(v[0], v[1], v[2], v[3]));
+    __stcs(p + 1, make_float4(v[4], v[5], v[6], v[7]));
+  } else {
+    __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + elem), pack8(v));
+  }
+}
 __device__ __forceinline__ void load_gain(const float* gain, int64_t elem, float (&g)[8]) {
   if (!gain) {
 #pragma unroll
