@@ -40,9 +40,24 @@ struct Args {
   float eps, per_elem;
 };
 
-// cosine and sine of p f, f a binary32 number: the product, its multiples of pi and what is left of a turn in 64 bits
-__device__ __forceinline__ float2 turn_of(int64_t p, float f) {
-  double t = (double)p * (double)f * 0.31830988618379067154;  // in half turns
+// What a CTA's warps read again and again
+struct Shared {
+  double per_turn[kMaxHalf];  // inverse frequencies over pi
+  float gain[2][256];         // of query and key heads
+  float2 table[kWarps][kMaxHalf];
+  __device__ __forceinline__ void fill(const Args& a) {
+    for (int i = threadIdx.x; i < a.half; i += kThreads) per_turn[i] = (double)a.inv_freq[i] * 0.31830988618379067154;
+    for (int i = threadIdx.x; i < a.dim; i += kThreads) {
+      gain[0][i] = a.gain_q ? a.gain_q[i] : 1.f;
+      gain[1][i] = a.gain_k ? a.gain_k[i] : 1.f;
+    }
+    for (int i = 2 * 256 - 1 - threadIdx.x; i >= 0; i -= kThreads)
+      if (i % 256 >= a.dim) gain[i / 256][i % 256] = 0.f;  // (of lanes beyond the head)
+  }
+};
+// cosine and sine of an angle of p f half turns: the product, its whole turns and what is left in 64 bits
+__device__ __forceinline__ float2 turn_of(double p, double f) {
+  double t = p * f;
   t -= 2. * rint(0.5 * t);
   float s, c;
   sincospif((float)t, &s, &c);
@@ -65,10 +80,11 @@ struct Lane {
   }
   __device__ __forceinline__ int element(int j) const { return e0 + (j < 2 ? 2 * j : gap + 2 * j - 4); }  // of pair j
   // the warp makes the row's table in shared memory and every lane takes what it needs of it
-  __device__ __forceinline__ void turn(const Args& a, float2* table, int64_t row) {
+  __device__ __forceinline__ void turn(const Args& a, Shared& sh, int64_t row) {
     if (MODE == kPlain) return;
-    const int64_t p = a.positions.p ? a.positions[row] : row;
-    for (int i = threadIdx.x & 31; i < a.half; i += 32) table[i] = turn_of(p, a.inv_freq[i]);
+    float2* const table = sh.table[threadIdx.x >> 5];
+    const double p = (double)(a.positions.p ? a.positions[row] : row);
+    for (int i = threadIdx.x & 31; i < a.half; i += 32) table[i] = turn_of(p, sh.per_turn[i]);
     __syncwarp();
     const float2 still = make_float2(1.f, 0.f);
 #pragma unroll
@@ -91,9 +107,9 @@ struct Lane {
   __device__ __forceinline__ static float2 partner(const float2 (&v)[4], int j) {
     return MODE == kHalves ? v[j ^ 2] : make_float2(v[j].y, v[j].x);
   }
-  __device__ __forceinline__ void load_gains(const float* gain, float2 (&g)[4]) const {
+  __device__ __forceinline__ void load_gains(const Shared& sh, int key, float2 (&g)[4]) const {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) g[j] = live && gain ? *reinterpret_cast<const float2*>(gain + element(j)) : both(1.f);
+    for (int j = 0; j < 4; ++j) g[j] = *reinterpret_cast<const float2*>(&sh.gain[key][element(j)]);
   }
   __device__ __forceinline__ void fetch(uint32_t dst, const uint16_t* p, bool there) const {
     if (MODE == kHalves) {
@@ -193,10 +209,10 @@ struct Walk {
   }
 };
 
-template <int G, int MODE, int N>
+template <int G, int MODE, int N, bool FULL>
 __global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a) {
   constexpr int kHeads = 32 / G, kStep = kHeads * N, kRing = kFwdRing<N>, kSlot = kThreads * 16 * N;  // heads of a step, bytes of a step of all warps
-  __shared__ float2 tables[kWarps][MODE == kPlain ? 1 : kMaxHalf];
+  __shared__ Shared sh;
   extern __shared__ __align__(16) uint8_t ring[];
   const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int64_t first = a.steps * w / warps;
@@ -210,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a)
     if (i < steps) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        const bool there = l.live && ahead.h + k * kHeads < ahead.heads(a);
+        const bool there = FULL || (l.live && ahead.h + k * kHeads < ahead.heads(a));
         l.fetch(mine + (i % kRing) * kSlot + k * (kThreads * 16), there ? from + k * head : a.x, there);
       }
       from += N * head;
@@ -220,18 +236,19 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a)
   };
   griddep_wait();
   griddep_launch_dependents();
-  if (steps == 0) return;
 #pragma unroll
   for (int u = 0; u < kRing - 1; ++u) fetch(u);
+  sh.fill(a);
+  __syncthreads();
   float2 gc[4], gs[4];
   int64_t turned = -1;  // the row whose rotation the lane has
   bool corner = true;
   for (int i = 0; i < steps; ++i) {
     if (corner) {
-      if (turned != at.row) l.turn(a, tables[threadIdx.x >> 5], at.row);
+      if (turned != at.row) l.turn(a, sh, at.row);
       turned = at.row;
       float2 g[4];
-      l.load_gains(at.key ? a.gain_k : a.gain_q, g);
+      l.load_gains(sh, at.key, g);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         gc[j] = MODE == kPlain ? g[j] : mul2(g[j], l.c[j]);
@@ -254,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a)
         if (MODE != kPlain) out[j] = fma2(l.partner(v[k], j), gs[j], out[j]);
         out[j] = mul2(out[j], both(rstd[k]));
       }
-      if (l.live && at.h + k * kHeads < at.heads(a)) l.store(to + k * head, out);
+      if (FULL || (l.live && at.h + k * kHeads < at.heads(a))) l.store(to + k * head, out);
     }
     to += N * head;
     corner = at.next(a, kStep, l.sub);
@@ -265,10 +282,10 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a)
 
 // A warp keeps the sums of its lanes' elements over all its steps in registers; at the end those of a CTA are added in a fixed
 // order and leave as a row of partial sums, which a second kernel adds.
-template <int G, int MODE, int N>
+template <int G, int MODE, int N, bool FULL>
 __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a) {
   constexpr int kHeads = 32 / G, kStep = kHeads * N, kRing = kBwdRing<N>, kSlot = kThreads * 32 * N;
-  __shared__ float2 tables[kWarps][MODE == kPlain ? 1 : kMaxHalf];
+  __shared__ Shared sh;
   extern __shared__ __align__(16) uint8_t ring[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + warp;
@@ -284,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a)
     if (i < steps) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
-        const bool there = l.live && ahead.h + k * kHeads < ahead.heads(a);
+        const bool there = FULL || (l.live && ahead.h + k * kHeads < ahead.heads(a));
         const uint32_t dst = mine + (i % kRing) * kSlot + k * (kThreads * 32);
         l.fetch(dst, there ? from_x + k * head : a.x, there);
         l.fetch(dst + kThreads * 16, there ? from_dy + k * head : a.dy, there);
@@ -302,6 +319,8 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a)
   griddep_launch_dependents();
 #pragma unroll
   for (int u = 0; u < kRing - 1; ++u) fetch(u);
+  sh.fill(a);
+  __syncthreads();
   // acc: of the kind of heads at hand; the other kind's wait in `other`
   float2 acc[4] = {}, other[4] = {}, gain[4];
   auto change = [&] {
@@ -317,9 +336,9 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a)
   bool corner = true;
   for (int i = 0; i < steps; ++i) {
     if (corner) {
-      if (turned != at.row) l.turn(a, tables[warp], at.row);
+      if (turned != at.row) l.turn(a, sh, at.row);
       turned = at.row;
-      l.load_gains(at.key ? a.gain_k : a.gain_q, gain);
+      l.load_gains(sh, at.key, gain);
       if (key != at.key) change();
       key = at.key;
     }
@@ -360,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a)
       float2 out[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) out[j] = mul2(fma2(n[k][j], both(-m[k] * a.per_elem), y[k][j]), both(r));
-      if (l.live && at.h + k * kHeads < at.heads(a)) l.store(to + k * head, out);
+      if (FULL || (l.live && at.h + k * kHeads < at.heads(a))) l.store(to + k * head, out);
     }
     to += N * head;
     corner = at.next(a, kStep, l.sub);
@@ -394,8 +413,8 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_bwd_kernel(const Args a)
   }
 }
 
-int lanes_of(int dim) {
-  int g = 1;
+int lanes_of(int dim) {  // (heads of less than 32 elements leave lanes idle)
+  int g = 4;
   while (g * 8 < dim) g *= 2;
   return g;
 }
@@ -426,9 +445,9 @@ Args args_of(const Heads& h, int n) {
   return a;
 }
 
-template <int G, int MODE, int N>
+template <int G, int MODE, int N, bool FULL>
 cudaError_t launch(bool bwd, const Args& a, cudaStream_t s) {
-  const auto kern = bwd ? headnorm_bwd_kernel<G, MODE, N> : headnorm_fwd_kernel<G, MODE, N>;
+  const auto kern = bwd ? headnorm_bwd_kernel<G, MODE, N, FULL> : headnorm_fwd_kernel<G, MODE, N, FULL>;
   const int smem = kThreads * N * (bwd ? kBwdRing<N> * 32 : kFwdRing<N> * 16);
   static std::atomic<uint64_t> configured[2]{};  // per instantiation and device
   int dev;
@@ -441,7 +460,10 @@ cudaError_t launch(bool bwd, const Args& a, cudaStream_t s) {
 }
 template <int G, int MODE>
 cudaError_t launch(bool bwd, int n, const Args& a, cudaStream_t s) {
-  return n == 2 ? launch<G, MODE, 2>(bwd, a, s) : launch<G, MODE, 1>(bwd, a, s);
+  const int of_step = n * (32 / G);
+  const bool full = a.dim == 8 * G && a.heads_q % of_step == 0 && a.heads_k % of_step == 0;  // no place of any step is empty
+  if (n == 2) return full ? launch<G, MODE, 2, true>(bwd, a, s) : launch<G, MODE, 2, false>(bwd, a, s);
+  return full ? launch<G, MODE, 1, true>(bwd, a, s) : launch<G, MODE, 1, false>(bwd, a, s);
 }
 template <int G>
 cudaError_t launch(bool bwd, bool interleaved, int n, const Args& a, cudaStream_t s) {
@@ -451,8 +473,6 @@ cudaError_t launch(bool bwd, bool interleaved, int n, const Args& a, cudaStream_
 cudaError_t launch(bool bwd, bool interleaved, int n, const Args& a, cudaStream_t s) {
   cudaError_t e;
   switch (lanes_of(a.dim)) {
-    case 1: e = launch<1>(bwd, interleaved, n, a, s); break;
-    case 2: e = launch<2>(bwd, interleaved, n, a, s); break;
     case 4: e = launch<4>(bwd, interleaved, n, a, s); break;
     case 8: e = launch<8>(bwd, interleaved, n, a, s); break;
     case 16: e = launch<16>(bwd, interleaved, n, a, s); break;
