@@ -67,6 +67,50 @@ def reduce_scatter_weight_grad(dW: torch.Tensor, out: torch.Tensor) -> None:
         out.copy_(dW.view_as(out))
 
 
+def allreduce_sq_norm(total: torch.Tensor) -> None:
+    """In-place FP64 sum over all ranks of the sums of squares of gradient shards (no-op without a process group): each rank
+    has its own rows' share (`reduce_scatter_weight_grad`), so that the norm of the whole gradient is the root of the total."""
+    assert total.dtype == torch.float64 and total.numel() == 1
+    if dist.is_available() and dist.is_initialized() and dist.get_world_size() > 1:
+        dist.all_reduce(total, op=dist.ReduceOp.SUM)
+
+
+class GradClipper:
+    """Clips the gradients of a step to a largest global norm, in place or into `outs` (the optimizer's buffers, bf16 or FP32).
+
+    sharded: the gradients are the rank's shards of a reduce-scatter, so that their sums of squares are added over the ranks in
+    between; gradients that were all-reduced are the same on every rank and need no exchange.  A gradient that ranks hold in
+    full beside sharded ones (a norm's gain, say) goes into `replicated`: it is counted on one rank only.  `stats` is {norm,
+    factor} on the device; a norm that is not finite gives the factor 0 and gradients of zeros."""
+
+    def __init__(self, grads, max_norm: float, outs=None, sharded: bool = False, replicated=(), replicated_outs=None):
+        from . import binding as B
+
+        self._B, self.max_norm, self.sharded = B, max_norm, sharded
+        grads, replicated = list(grads), list(replicated)
+        device = (grads + replicated)[0].device
+        both_outs = None
+        if outs is not None or replicated_outs is not None:
+            both_outs = list(outs if outs is not None else grads) + list(replicated_outs if replicated_outs is not None else replicated)
+        self._all = B.grad_list(grads + replicated, both_outs)
+        rank = dist.get_rank() if dist.is_available() and dist.is_initialized() else 0
+        counted = grads + (replicated if rank == 0 or not sharded else [])
+        self._counted = B.grad_list(counted) if counted else None
+        self.total = torch.zeros(1, dtype=torch.float64, device=device)
+        self.stats = torch.empty(2, dtype=torch.float32, device=device)
+        self._workspace = torch.empty(B.nvfp4_grad_sq_norm_workspace_bytes(), dtype=torch.uint8, device=device)
+
+    def __call__(self) -> torch.Tensor:
+        if self._counted is None:
+            self.total.zero_()
+        else:
+            self._B.nvfp4_grad_sq_norm(self._counted, self.total, self._workspace)
+        if self.sharded:
+            allreduce_sq_norm(self.total)
+        self._B.nvfp4_grad_clip(self._all, self.total, self.max_norm, self.stats)
+        return self.stats
+
+
 class OverlappedGradExchange:
     """Weight-gradient buffers whose exchange runs beside the next step's kernels.
 
