@@ -20,7 +20,6 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
 constexpr int kRing = 5, kStage = kThreads * 32;  // what is on its way to a CTA: 32 bytes a thread and stage
-constexpr int kShortRow = 4096;                   // up to here a warp takes a row by itself
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kLowest = -3.402823466e38f, kFar = -300.f, kReach = 400.f;
 
 __device__ __forceinline__ float exp2_fast(float v) {
@@ -284,7 +283,7 @@ struct Partial {
   float m, s, t;
 };
 
-// W warps to a row: one (up to kShortRow columns; a CTA has kWarps rows), or a CTA, or a cluster of gridDim.y CTAs, each with a run of the row's
+// W warps to a row: one (see warp_rows(); a CTA has kWarps rows), or a CTA, or a cluster of gridDim.y CTAs, each with a run of the row's
 // sixteen-byte chunks, whose findings the first one joins.
 template <bool F32, bool ENTROPY, bool TOP, int W>
 __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
@@ -615,6 +614,11 @@ unsigned cluster_of(int64_t rows, int64_t vocab) {
   return n;
 }
 
+// Whether a warp takes a row by itself: it has no barriers to wait at, and takes longer by the row's length.  By one warp / by a CTA, us: 512 x 4096 4.2 / 4.2, 512 x 8192
+// 5.9 / 5.1; 2048 x 8192 9.7 / 14.6, 2048 x 32768 26.3 / 28.4, 16384 x 1000 13.4 / 74, 16384 x 32768 166 / 193; with the likeliest tokens 2048 x 8192 21 / 30,
+// 2048 x 16384 38 / 35, 16384 x 16384 151 / 256, 16384 x 32768 345 / 310.
+bool warp_rows(int64_t rows, int64_t vocab, bool top) { return vocab <= 4096 || (rows >= 2048 && vocab <= (top ? 16384 : 32768)); }
+
 template <typename K>
 cudaError_t configure(K kern, size_t smem, std::atomic<uint64_t>& configured) {
   int dev;
@@ -636,7 +640,7 @@ cudaError_t launch_fwd(const Fwd& a, unsigned ctas, cudaStream_t s) {
 }
 template <bool F32, bool ENTROPY, bool TOP>
 cudaError_t launch_fwd(const Fwd& a, cudaStream_t s) {
-  if (a.vocab <= kShortRow) return launch_fwd<F32, ENTROPY, TOP, 1>(a, 1, s);
+  if (warp_rows(a.rows, a.vocab, TOP)) return launch_fwd<F32, ENTROPY, TOP, 1>(a, 1, s);
   return launch_fwd<F32, ENTROPY, TOP, kWarps>(a, cluster_of(a.rows, a.vocab), s);
 }
 template <bool F32, bool OUT32>
