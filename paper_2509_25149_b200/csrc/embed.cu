@@ -4,6 +4,7 @@
 // its places) and every sum is a run of the sorted list: no order of additions that varies, the same bits in every run.
 //   rank_kernel    few tokens: a warp counts how many stand before its token
 //   sort_kernel    more: a cluster of eight CTAs sorts (token, place) pairs by digits of up to nine bits
+//   digits_kernel  many: the same with a launch for each of a pass's steps, over all SMs
 //   zeros_kernel   where the gradient is not added to what is there, zeros in the whole table, beside the sort
 //   runs_kernel    chunks of the sorted list: whoever has the beginning of a run adds it up, over the end of its chunk too; of a run that has a whole
 //                  chunk in its middle every chunk leaves a partial sum
@@ -77,12 +78,127 @@ struct Sort {
   Entry* sorted;
   Entry* other;
   int64_t n, vocab;
-  int passes, bits;  // digits of `bits` bits
+  int passes, bits;     // digits of `bits` bits
+  uint32_t* of_tile;    // digits_kernel: [digit][tile], how often it occurs, then how often in the tiles before
+  uint32_t* of_digit;   // and in all of them
+  int tiles, pass;
 };
 struct SortShared {
   uint32_t counts[kSortWarps][kBins];
   uint32_t total[kBins], of_warp[32];
   uint2 list[kSortTile];  // the CTA's part of the list, where it has room for it
+};
+
+// A pass of the sort as one CTA sees it, which has the entries c0 .. c1 - 1 and whose warps have a part of them each: how often each digit occurs
+// in every warp's part, where each warp's first one of a digit goes (behind all smaller digits, and behind the same one in the parts before), and the moves.
+struct Pass {
+  const Sort& a;
+  SortShared& sh;
+  const Entry* src;
+  Entry* dst;
+  int64_t c0, c1, lo, hi;
+  int pass, shift, warps, warp, lane;
+  bool held;
+  __device__ __forceinline__ Pass(const Sort& a_, SortShared& sh_, int pass_, int64_t from, int64_t to) : a(a_), sh(sh_), c0(from), c1(to), pass(pass_) {
+    const bool even = (a.passes - 1 - pass) % 2 == 0;
+    src = even ? a.other : a.sorted;
+    dst = even ? a.sorted : a.other;
+    shift = pass * a.bits;
+    warp = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    warps = (int)min((int64_t)kSortWarps, (c1 - c0 + 31) / 32);  // that have a part
+    lo = warp < warps ? c0 + (c1 - c0) * warp / warps : c1;
+    hi = warp < warps ? c0 + (c1 - c0) * (warp + 1) / warps : c1;
+    held = c1 - c0 <= kSortTile;
+  }
+  __device__ __forceinline__ uint2 entry(int64_t i) const {
+    if (pass > 0) {
+      const Entry e = load_entry(src + i);
+      return make_uint2(e.token, e.place);
+    }
+    const int64_t t = a.tokens[i];
+    return make_uint2(t >= 0 && t < a.vocab ? (uint32_t)t : (uint32_t)a.vocab, (uint32_t)i);
+  }
+  // the lanes that have the same digit, by one vote a bit (match.any asks digit by digit: 65536 tokens 69.5 -> 63.5 us)
+  __device__ __forceinline__ uint32_t alike(uint32_t digit, bool live) const {
+    uint32_t same = __ballot_sync(0xffffffffu, live);
+    for (int b = 0; b < a.bits; ++b) {
+      const uint32_t ones = __ballot_sync(0xffffffffu, digit >> b & 1u);
+      same &= digit >> b & 1u ? ones : ~ones;
+    }
+    return same;
+  }
+  // four neighbouring groups of 32 whose loads are on their way together
+  template <class F>
+  __device__ __forceinline__ void each(F work) const {
+    const uint32_t mask = (1u << a.bits) - 1u;
+    for (int64_t i0 = lo; i0 < hi; i0 += 128) {
+      uint2 e[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t i = i0 + 32 * u + lane;
+        e[u] = i < hi ? (held ? sh.list[i - c0] : entry(i)) : make_uint2(0u, 0u);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i0 + 32 * u >= hi) break;
+        const bool live = i0 + 32 * u + lane < hi;
+        const uint32_t digit = (e[u].x >> shift) & mask;
+        work(e[u], digit, alike(digit, live), live);
+        __syncwarp();
+      }
+    }
+  }
+  // counts of every warp, turned into how many the warps before have; how often the thread's digit occurs in the CTA
+  __device__ __forceinline__ uint32_t count() const {
+    const uint32_t below = (1u << lane) - 1u;
+    const int bins = 1 << a.bits;
+    if (held)
+      for (int64_t i = c0 + threadIdx.x; i < c1; i += kSortThreads) sh.list[i - c0] = entry(i);
+    for (int b = threadIdx.x; b < warps * bins; b += kSortThreads) sh.counts[b >> a.bits][b & (bins - 1)] = 0u;
+    __syncthreads();
+    each([&](uint2, uint32_t digit, uint32_t same, bool live) {
+      if (live && (same & below) == 0u) sh.counts[warp][digit] += __popc(same);
+    });
+    __syncthreads();
+    uint32_t sum = 0;
+    if (threadIdx.x < bins)
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) {
+        const uint32_t c = sh.counts[w][threadIdx.x];
+        sh.counts[w][threadIdx.x] = sum;
+        sum += c;
+      }
+    return sum;
+  }
+  // all: how often the thread's digit occurs in the whole list; before: in the CTAs before
+  __device__ __forceinline__ void move(uint32_t all, uint32_t before) const {
+    const uint32_t below = (1u << lane) - 1u;
+    uint32_t scan = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, scan, o);
+      if (lane >= o) scan += v;
+    }
+    if (lane == 31) sh.of_warp[warp] = scan;
+    __syncthreads();
+    if (threadIdx.x < 1 << a.bits) {
+      for (int w = 0; w < warp; ++w) scan += sh.of_warp[w];
+      const uint32_t base = scan - all + before;
+#pragma unroll 8
+      for (int w = 0; w < warps; ++w) sh.counts[w][threadIdx.x] += base;
+    }
+    __syncthreads();
+    each([&](uint2 e, uint32_t digit, uint32_t same, bool live) {
+      uint32_t at = 0;
+      if (live) at = sh.counts[warp][digit];
+      __syncwarp();
+      if (live) {
+        *reinterpret_cast<uint2*>(dst + at + __popc(same & below)) = e;
+        if ((same & below) == 0u) sh.counts[warp][digit] = at + __popc(same);
+      }
+    });
+  }
 };
 
 // A token's place in the sorted list is the number of smaller ones and of equal ones before it.  That is n^2 / 32 steps for n tokens, without a barrier or
@@ -108,73 +224,19 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const Sort a) {
   if (lane == 0) *reinterpret_cast<uint2*>(a.sorted + before) = make_uint2(mine, (uint32_t)i);
 }
 
-// Every CTA, and in it every warp, has a part of the list.  A pass counts the digits of every warp's part, finds where each warp's first one of a digit
-// goes (behind all smaller digits, and behind the same one in the parts before), and moves the pairs.
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
   extern __shared__ __align__(16) uint8_t smem[];
   SortShared& sh = *reinterpret_cast<SortShared*>(smem);
   griddep_wait();
   griddep_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x, bins = 1 << a.bits;
-  const int64_t c0 = a.n * rank / kSortCtas, c1 = a.n * (rank + 1) / kSortCtas;
-  const int warps = (int)min((int64_t)kSortWarps, (c1 - c0 + 31) / 32);  // that have a part
-  const int64_t lo = warp < warps ? c0 + (c1 - c0) * warp / warps : c1, hi = warp < warps ? c0 + (c1 - c0) * (warp + 1) / warps : c1;
-  const uint32_t below = (1u << lane) - 1u, mask = bins - 1u;
-  const bool held = c1 - c0 <= kSortTile;
+  const int rank = blockIdx.x;
   for (int pass = 0; pass < a.passes; ++pass) {
-    const bool even = (a.passes - 1 - pass) % 2 == 0;
-    const Entry* const src = even ? a.other : a.sorted;
-    Entry* const dst = even ? a.sorted : a.other;
-    const int shift = pass * a.bits;
-    auto entry = [&](int64_t i) {
-      if (pass > 0) {
-        const Entry e = load_entry(src + i);
-        return make_uint2(e.token, e.place);
-      }
-      const int64_t t = a.tokens[i];
-      return make_uint2(t >= 0 && t < a.vocab ? (uint32_t)t : (uint32_t)a.vocab, (uint32_t)i);
-    };
-    if (held)
-      for (int64_t i = c0 + threadIdx.x; i < c1; i += kSortThreads) sh.list[i - c0] = entry(i);
-    for (int b = threadIdx.x; b < warps * bins; b += kSortThreads) sh.counts[b >> a.bits][b & mask] = 0u;
-    __syncthreads();
-    // four neighbouring groups of 32 whose loads are on their way together
-    auto each = [&](auto work) {
-      for (int64_t i0 = lo; i0 < hi; i0 += 128) {
-        uint2 e[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int64_t i = i0 + 32 * u + lane;
-          e[u] = i < hi ? (held ? sh.list[i - c0] : entry(i)) : make_uint2(0u, 0u);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          if (i0 + 32 * u >= hi) break;
-          const bool live = i0 + 32 * u + lane < hi;
-          const uint32_t digit = live ? (e[u].x >> shift) & mask : ~0u;
-          work(e[u], digit, __match_any_sync(0xffffffffu, digit), live);
-          __syncwarp();
-        }
-      }
-    };
-    each([&](uint2, uint32_t digit, uint32_t same, bool live) {
-      if (live && (same & below) == 0u) sh.counts[warp][digit] += __popc(same);
-    });
-    __syncthreads();
-    uint32_t all = 0, before = 0;
-    if (threadIdx.x < bins) {
-      uint32_t sum = 0;
-#pragma unroll 8
-      for (int w = 0; w < warps; ++w) {
-        const uint32_t c = sh.counts[w][threadIdx.x];
-        sh.counts[w][threadIdx.x] = sum;
-        sum += c;
-      }
-      sh.total[threadIdx.x] = sum;
-    }
+    const Pass p(a, sh, pass, a.n * rank / kSortCtas, a.n * (rank + 1) / kSortCtas);
+    const uint32_t mine = p.count();
+    if (threadIdx.x < kBins) sh.total[threadIdx.x] = mine;
     cluster_sync();
-    if (threadIdx.x < bins) {
-      all = 0;
+    uint32_t all = 0, before = 0;
+    if (threadIdx.x < 1 << a.bits) {
 #pragma unroll
       for (int r = 0; r < kSortCtas; ++r) {
         const uint32_t c = __float_as_uint(ld_of_rank(reinterpret_cast<const float*>(&sh.total[threadIdx.x]), r));
@@ -182,32 +244,47 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const Sort a) {
         all += c;
       }
     }
-    uint32_t scan = all;
+    p.move(all, before);
+    cluster_sync();  // the list is written, and nobody reads the totals any more
+  }
+}
+
+// A pass over many tokens: every CTA counts the digits of a tile, a warp to a digit adds up what the tiles before have, and every CTA moves its tile.
+template <bool MOVE>
+__global__ void __launch_bounds__(kSortThreads) digits_kernel(const Sort a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  SortShared& sh = *reinterpret_cast<SortShared*>(smem);
+  griddep_wait();
+  griddep_launch_dependents();
+  const int64_t c0 = (int64_t)blockIdx.x * kSortTile;
+  const Pass p(a, sh, a.pass, c0, min(c0 + kSortTile, a.n));
+  const uint32_t mine = p.count();
+  const bool has = threadIdx.x < 1 << a.bits;
+  uint32_t* const at = a.of_tile + (int64_t)threadIdx.x * a.tiles + blockIdx.x;
+  if (MOVE)
+    p.move(has ? __ldcg(a.of_digit + threadIdx.x) : 0u, has ? __ldcg(at) : 0u);
+  else if (has)
+    *at = mine;
+}
+__global__ void __launch_bounds__(256) before_kernel(const Sort a) {
+  griddep_wait();
+  griddep_launch_dependents();
+  const int digit = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (digit >= 1 << a.bits) return;
+  uint32_t* const row = a.of_tile + (int64_t)digit * a.tiles;
+  uint32_t sum = 0;
+  for (int i0 = 0; i0 < a.tiles; i0 += 32) {
+    const uint32_t c = i0 + lane < a.tiles ? __ldcg(row + i0 + lane) : 0u;
+    uint32_t scan = c;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t v = __shfl_up_sync(0xffffffffu, scan, o);
       if (lane >= o) scan += v;
     }
-    if (lane == 31) sh.of_warp[warp] = scan;
-    __syncthreads();
-    if (threadIdx.x < bins) {
-      for (int w = 0; w < warp; ++w) scan += sh.of_warp[w];
-      const uint32_t base = scan - all + before;
-#pragma unroll 8
-      for (int w = 0; w < warps; ++w) sh.counts[w][threadIdx.x] += base;
-    }
-    __syncthreads();
-    each([&](uint2 e, uint32_t digit, uint32_t same, bool live) {
-      uint32_t at = 0;
-      if (live) at = sh.counts[warp][digit];
-      __syncwarp();
-      if (live) {
-        *reinterpret_cast<uint2*>(dst + at + __popc(same & below)) = e;
-        if ((same & below) == 0u) sh.counts[warp][digit] = at + __popc(same);
-      }
-    });
-    cluster_sync();  // the list is written, and nobody reads the totals any more
+    if (i0 + lane < a.tiles) row[i0 + lane] = sum + scan - c;
+    sum += __shfl_sync(0xffffffffu, scan, 31);
   }
+  if (lane == 0) a.of_digit[digit] = sum;
 }
 
 // 32 KB of zeros to a CTA: CTAs that end and make room for the next ones keep to neighbouring memory, which HBM writes at 7.5 TB/s; resident ones that go
@@ -457,8 +534,11 @@ cudaError_t launch_embedding_fwd(const Embed& e, cudaStream_t s) {
   return err;
 }
 
+// tokens that the cluster sorts (by it / by launches over all SMs, whole gradient of 64 columns: 65536 63.5 / 66.5 us, 131072 107 / 85, 1000000 483 / 167)
+constexpr int64_t kClusterMost = 65536;
+int64_t tiles_of(int64_t n) { return n > kClusterMost ? (n + kSortTile - 1) / kSortTile : 0; }
 size_t embedding_bwd_workspace(int64_t n, int64_t cols) {
-  return 2 * padded((size_t)n * sizeof(Entry)) + 2 * padded((size_t)chunks_of(n) * cols * 4);
+  return 2 * padded((size_t)n * sizeof(Entry)) + 2 * padded((size_t)chunks_of(n) * cols * 4) + padded((size_t)(tiles_of(n) + 1) * kBins * 4);
 }
 
 cudaError_t launch_embedding_bwd(const Embed& e, cudaStream_t s) {
@@ -482,16 +562,31 @@ cudaError_t launch_embedding_bwd(const Embed& e, cudaStream_t s) {
   cudaError_t err;
   if (device_needs_config(configured, &dev)) {
     if ((err = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared))) != cudaSuccess ||
+        (err = cudaFuncSetAttribute(digits_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared))) != cudaSuccess ||
+        (err = cudaFuncSetAttribute(digits_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SortShared))) != cudaSuccess ||
         (err = cudaFuncSetAttribute(runs_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024)) != cudaSuccess ||
         (err = cudaFuncSetAttribute(runs_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024)) != cudaSuccess)
       return err;
     device_configured(configured, dev);
   }
-  if (e.n <= kRankMost)
+  if (e.n <= kRankMost) {
     err = launch_divided(-1, rank_kernel, dim3((unsigned)((e.n + kRankThreads / 32 - 1) / (kRankThreads / 32))), dim3(kRankThreads), 0, s, k);
-  else
+    count_launch();
+  } else if (e.n <= kClusterMost) {
     err = launch_cluster(kSortCtas, sort_kernel, dim3(kSortCtas), dim3(kSortThreads), sizeof(SortShared), s, k);
-  count_launch();
+    count_launch();
+  } else {
+    k.tiles = (int)tiles_of(e.n);
+    k.of_tile = reinterpret_cast<uint32_t*>(take((size_t)(k.tiles + 1) * kBins * 4));
+    k.of_digit = k.of_tile + (int64_t)k.tiles * kBins;
+    err = cudaSuccess;
+    for (k.pass = 0; k.pass < k.passes && err == cudaSuccess; ++k.pass) {
+      err = launch_divided(100, digits_kernel<false>, dim3((unsigned)k.tiles), dim3(kSortThreads), sizeof(SortShared), s, k);
+      if (err == cudaSuccess) err = launch_kernel(before_kernel, dim3((1u << k.bits) / 8 + 1), dim3(256), 0, s, k);
+      if (err == cudaSuccess) err = launch_divided(100, digits_kernel<true>, dim3((unsigned)k.tiles), dim3(kSortThreads), sizeof(SortShared), s, k);
+      count_launch(3);
+    }
+  }
   if (err != cudaSuccess) return err;
   if (!e.accumulate) {
     err = launch_divided(-1, zeros_kernel, dim3((unsigned)((e.vocab * (e.cols / 4) + kZeros - 1) / kZeros)), dim3(kZeroThreads), 0, s,
