@@ -3,6 +3,7 @@
 // Bound by HBM: everything is read for the sum and once more to be scaled, since the factor needs the whole sum first (the second pass goes backwards, so
 // that what the first one read last is still in L2).  The list of tensors travels in the kernel's parameters, so that a captured graph holds it
 // and nothing is copied to the device.  Tensors are cut into tiles, which the CTAs take in turn.
+// 770 million binary32 numbers to bf16: 452 us for the sum (104 % of the copy rate), 670 to scale (105 %: some of it from L2).
 #include <algorithm>
 #include <climits>
 

@@ -8,6 +8,8 @@
 // share.  What a lane is going to need comes by cp.async through a ring in shared memory in which every thread has places of its own, so that loads
 // stay in flight whatever the registers hold and over the end of a row.  Sine and cosine of a row's angles are the same for all its heads: the warp makes them once a row, the angle in 64 bits (a far position
 // times a frequency has its last bits below binary32), and keeps them in shared memory.
+// 8192 rows of 40 + 8 heads of 128: 39.2 us (79 % of the copy rate) and 59 with 4.3 for the sums of the gains' gradients (78 %).  What they wait for is latency: 94 and 155
+// instructions a lane for eight elements, shuffles behind one another; 24 warps an SM with one head to a lane took 41 and 65.
 #include <algorithm>
 
 #include "around.h"
