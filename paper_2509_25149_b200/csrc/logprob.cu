@@ -72,7 +72,6 @@ template <bool F32>
 struct Chunk {
   static constexpr int E = F32 ? 4 : 8, kPairs = E / 2;
   uint4 w;
-  __device__ __forceinline__ void nothing() { w.x = w.y = w.z = w.w = F32 ? 0xff800000u : 0xff80ff80u; }  // minus infinities
   __device__ __forceinline__ void load(const void* row, int64_t c) { w = ldg128_stream(static_cast<const uint8_t*>(row) + c * 16); }
   __device__ __forceinline__ void values(float2* v) const {
     if (F32) {
