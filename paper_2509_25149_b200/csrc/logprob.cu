@@ -513,7 +513,8 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const Bwd a) {
   constexpr int E = Chunk<F32>::E, kSlots = kRing * 2, kSlot = kThreads * 16;
   extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31;
-  const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5), first = a.steps * w / warps;
+  // (the last rows first: of what the forward pass read last some is still in L2)
+  const int64_t warps = (int64_t)gridDim.x * kWarps, w = (int64_t)(gridDim.x - 1 - blockIdx.x) * kWarps + (threadIdx.x >> 5), first = a.steps * w / warps;
   const int steps = (int)(a.steps * (w + 1) / warps - first), whole = (int)(a.vocab / E), of_row = (int)a.per_row * 32;
   const uint32_t mine = smem_u32(smem) + threadIdx.x * 16;
   int64_t row = first / a.per_row;
