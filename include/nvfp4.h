@@ -440,7 +440,8 @@ NVFP4_API nvfp4_status nvfp4_embedding_bwd(const void* tokens, int32_t tokens_ar
  *   would not hold the sum beside a large logit).
  *   top_ids (int32), top_logprobs (binary32): [rows x top], the `top` likeliest tokens, likeliest first, equal ones by index; 1 <= top <=
  *   NVFP4_TOP_MAX and <= vocab where either is wanted.
- *   A row of nothing but minus infinities has lse and log probabilities of minus infinity and entropy 0.
+ *   A row of nothing but minus infinities has lse and log probabilities of minus infinity and entropy 0; one with a NaN has NaN in all but the
+ *   likeliest tokens' numbers, which are some of [0, vocab), and in its gradient.
  * nvfp4_logprob_bwd: the gradient of sum over rows of dlogprob * logprob + dentropy * entropy by the logits:
  *   dlogits = scale * (dlogprob * ((j == target) - p) - dentropy * p * (log p + entropy)), in the type of the logits or the other one (dlogits_is_fp32),
  *   the columns from vocab to dcols (>= vocab: what the product behind it reads) set to zero.

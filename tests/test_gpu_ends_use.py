@@ -330,3 +330,54 @@ def test_gradients_beyond_2_31():
     assert float(total) == 0.25 * (n - 1) + 9.0
     B.nvfp4_grad_clip(held, total, math.sqrt(float(total)) * 0.5, stats)
     assert abs(float(stats[1]) - 0.5) < 1e-6 and float(g[-1]) == 1.5 and bool((g[:-1] == 0.25).all())
+
+
+# ------------------------------------------------------------------------------------------------- what is refused ----
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=str)
+@pytest.mark.parametrize("vocab", [1000, 9000, 40000])
+def test_a_nan_logit_spoils_its_row_and_no_other(vocab, dtype):
+    x = normal((6, vocab), 1, 2.0, dtype)
+    x[2, vocab // 3] = math.nan
+    x[4, vocab - 1] = -math.nan
+    z, tg, w = x.cuda(), torch.arange(6, device="cuda"), torch.ones(6, device="cuda")
+    lp, lse, st, en, dz = new(6), new(6), new(6, 2), new(6), torch.empty_like(z)
+    ids, tops = new(6, 5, dtype=torch.int32), new(6, 5)
+    B.nvfp4_logprob_fwd(z, tg, lp, lse, st, en, ids, tops)
+    B.nvfp4_logprob_bwd(z, tg, st, dz, w, en, w)
+    bad = torch.tensor([False, False, True, False, True, False], device="cuda")
+    for t in (lp, lse, en):
+        assert torch.equal(torch.isnan(t), bad)
+    assert bool(torch.isnan(dz[bad]).all()) and bool(torch.isfinite(dz[~bad]).all()) and bool(torch.isfinite(tops[~bad]).all())
+    assert int(ids.min()) >= 0 and int(ids.max()) < vocab
+    good = x[[0, 1, 3, 5]]
+    assert torch.equal(ids[~bad].cpu().long(), R.top_of(good, 5))
+
+
+def test_the_bindings_refuse_what_they_cannot_take():
+    x, f = torch.zeros(4, 384, dtype=BF16, device="cuda"), torch.ones(32, device="cuda")
+    tok, tab = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(9, 384, device="cuda")
+    z, lse, total = torch.zeros(4, 37, device="cuda"), new(4), new(1, dtype=torch.float64)
+    ws = scratch(1 << 16)
+    before = B.nvfp4_launch_count()
+    for call in (lambda: B.nvfp4_headnorm_fwd(x, 4, 1, x),  # 384 columns are not five heads
+                 lambda: B.nvfp4_headnorm_fwd(x.float(), 4, 2, x), lambda: B.nvfp4_headnorm_fwd(x, 4, 2, x.t()),
+                 lambda: B.nvfp4_headnorm_fwd(x, 4, 2, x, inv_freq=f.cpu()), lambda: B.nvfp4_headnorm_fwd(x, 4, 2, x, positions=tok[:3]),
+                 lambda: B.nvfp4_headnorm_fwd(x, 4, 2, x, gain_q=torch.ones(63, device="cuda")), lambda: B.nvfp4_headnorm_fwd(x.cpu(), 4, 2, x),
+                 lambda: B.nvfp4_embedding_fwd(tok.float(), tab, x), lambda: B.nvfp4_embedding_fwd(tok, tab, x[:3]), lambda: B.nvfp4_embedding_fwd(tok[::2], tab, x[:2]),
+                 lambda: B.nvfp4_embedding_bwd(tok, x, tab.bfloat16(), ws), lambda: B.nvfp4_embedding_bwd(tok, x, tab.cpu(), ws),
+                 lambda: B.nvfp4_logprob_fwd(z.half(), lse=lse), lambda: B.nvfp4_logprob_fwd(z, lse=lse[:3]), lambda: B.nvfp4_logprob_fwd(z, tok[:2], lse),
+                 lambda: B.nvfp4_logprob_fwd(z, top_ids=new(4, 3, dtype=torch.int64)), lambda: B.nvfp4_logprob_fwd(z, top_ids=new(4, 3, dtype=torch.int32), top_logprobs=new(4, 2)),
+                 lambda: B.nvfp4_logprob_bwd(z, tok, new(4, 1), z, lse), lambda: B.nvfp4_logprob_bwd(z, tok, new(4, 2), z[:, :3].clone()[:2], lse),
+                 lambda: B.grad_list([x.half()]), lambda: B.grad_list([x.t()]), lambda: B.grad_list([x, x.cpu()]), lambda: B.grad_list([x], [x[:2]]),
+                 lambda: B.nvfp4_grad_sq_norm(B.grad_list([x]), new(1), ws)):
+        with pytest.raises(AssertionError):
+            call()
+    for status, call in ((3, lambda: B.nvfp4_logprob_fwd(z, lse=lse)),  # rows 37 elements apart
+                         (2, lambda: B.nvfp4_headnorm_fwd(x, 4, 2, x, inv_freq=torch.ones(36, device="cuda"))), (2, lambda: B.nvfp4_headnorm_fwd(x, 1, 0, x)),
+                         (4, lambda: B.nvfp4_headnorm_fwd(x, 4, 2, x, eps=0.0)), (5, lambda: B.nvfp4_embedding_bwd(tok, x, tab, ws[:256])),
+                         (2, lambda: B.nvfp4_logprob_fwd(new(4, 40), top_ids=new(4, 33, dtype=torch.int32))), (5, lambda: B.nvfp4_grad_sq_norm(B.grad_list([x]), total, ws[:256])),
+                         (4, lambda: B.nvfp4_grad_clip(B.grad_list([x]), total, 0.0))):
+        with pytest.raises(B.NVFP4Error) as e:
+            call()
+        assert e.value.status == status
+    assert B.nvfp4_launch_count() == before
