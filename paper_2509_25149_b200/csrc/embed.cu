@@ -86,30 +86,30 @@ struct Sort {
 struct SortShared {
   uint32_t counts[kSortWarps][kBins];
   uint32_t total[kBins], of_warp[32];
-  uint2 list[kSortTile];  // the CTA's part of the list, where it has room for it
+  uint2 list[kSortTile];       // the CTA's part of the list
+  uint16_t place[kSortTile];  // how many of an entry's warp have its digit and stand before it
 };
 
-// A pass of the sort as one CTA sees it, which has the entries c0 .. c1 - 1 and whose warps have a part of them each: how often each digit occurs
-// in every warp's part, where each warp's first one of a digit goes (behind all smaller digits, and behind the same one in the parts before), and the moves.
+// A pass of the sort as one CTA sees it, which has the entries c0 .. c1 - 1, kSortTile at most, and whose warps have a part of them each: how often each digit
+// occurs in every warp's part, where each warp's first one of a digit goes (behind all smaller digits, and behind the same one in the parts before), and the
+// moves, in which an entry's place is known.
 struct Pass {
   const Sort& a;
   SortShared& sh;
   const Entry* src;
   Entry* dst;
-  int64_t c0, c1, lo, hi;
-  int pass, shift, warps, warp, lane;
-  bool held;
-  __device__ __forceinline__ Pass(const Sort& a_, SortShared& sh_, int pass_, int64_t from, int64_t to) : a(a_), sh(sh_), c0(from), c1(to), pass(pass_) {
+  int64_t c0;
+  int size, part, pass, shift, warps, warp, lane;  // part: entries of a warp
+  __device__ __forceinline__ Pass(const Sort& a_, SortShared& sh_, int pass_, int64_t from, int64_t to)
+      : a(a_), sh(sh_), c0(from), size((int)(to - from)), pass(pass_) {
     const bool even = (a.passes - 1 - pass) % 2 == 0;
     src = even ? a.other : a.sorted;
     dst = even ? a.sorted : a.other;
     shift = pass * a.bits;
     warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
-    warps = (int)min((int64_t)kSortWarps, (c1 - c0 + 31) / 32);  // that have a part
-    lo = warp < warps ? c0 + (c1 - c0) * warp / warps : c1;
-    hi = warp < warps ? c0 + (c1 - c0) * (warp + 1) / warps : c1;
-    held = c1 - c0 <= kSortTile;
+    part = ((size + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
+    warps = (size + part - 1) / part;
   }
   __device__ __forceinline__ uint2 entry(int64_t i) const {
     if (pass > 0) {
@@ -119,7 +119,8 @@ struct Pass {
     const int64_t t = a.tokens[i];
     return make_uint2(t >= 0 && t < a.vocab ? (uint32_t)t : (uint32_t)a.vocab, (uint32_t)i);
   }
-  // the lanes that have the same digit, by one vote a bit (match.any asks digit by digit: 65536 tokens 69.5 -> 63.5 us)
+  __device__ __forceinline__ uint32_t digit_of(uint2 e) const { return (e.x >> shift) & ((1u << a.bits) - 1u); }
+  // the lanes that have the same digit, by one vote a bit (match.any asks digit by digit, 10 % of the whole)
   __device__ __forceinline__ uint32_t alike(uint32_t digit, bool live) const {
     uint32_t same = __ballot_sync(0xffffffffu, live);
     for (int b = 0; b < a.bits; ++b) {
@@ -128,38 +129,25 @@ struct Pass {
     }
     return same;
   }
-  // four neighbouring groups of 32 whose loads are on their way together
-  template <class F>
-  __device__ __forceinline__ void each(F work) const {
-    const uint32_t mask = (1u << a.bits) - 1u;
-    for (int64_t i0 = lo; i0 < hi; i0 += 128) {
-      uint2 e[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t i = i0 + 32 * u + lane;
-        e[u] = i < hi ? (held ? sh.list[i - c0] : entry(i)) : make_uint2(0u, 0u);
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (i0 + 32 * u >= hi) break;
-        const bool live = i0 + 32 * u + lane < hi;
-        const uint32_t digit = (e[u].x >> shift) & mask;
-        work(e[u], digit, alike(digit, live), live);
-        __syncwarp();
-      }
-    }
-  }
   // counts of every warp, turned into how many the warps before have; how often the thread's digit occurs in the CTA
   __device__ __forceinline__ uint32_t count() const {
     const uint32_t below = (1u << lane) - 1u;
     const int bins = 1 << a.bits;
-    if (held)
-      for (int64_t i = c0 + threadIdx.x; i < c1; i += kSortThreads) sh.list[i - c0] = entry(i);
+    for (int i = threadIdx.x; i < size; i += kSortThreads) sh.list[i] = entry(c0 + i);
     for (int b = threadIdx.x; b < warps * bins; b += kSortThreads) sh.counts[b >> a.bits][b & (bins - 1)] = 0u;
     __syncthreads();
-    each([&](uint2, uint32_t digit, uint32_t same, bool live) {
-      if (live && (same & below) == 0u) sh.counts[warp][digit] += __popc(same);
-    });
+    for (int i0 = warp * part; i0 < min((warp + 1) * part, size); i0 += 32) {
+      const bool live = i0 + lane < size;
+      const uint32_t digit = live ? digit_of(sh.list[i0 + lane]) : 0u, same = alike(digit, live);
+      uint32_t before = 0;
+      if (live) before = sh.counts[warp][digit];
+      __syncwarp();
+      if (live) {
+        sh.place[i0 + lane] = (uint16_t)(before + __popc(same & below));
+        if ((same & below) == 0u) sh.counts[warp][digit] = before + __popc(same);
+      }
+      __syncwarp();
+    }
     __syncthreads();
     uint32_t sum = 0;
     if (threadIdx.x < bins)
@@ -173,7 +161,6 @@ struct Pass {
   }
   // all: how often the thread's digit occurs in the whole list; before: in the CTAs before
   __device__ __forceinline__ void move(uint32_t all, uint32_t before) const {
-    const uint32_t below = (1u << lane) - 1u;
     uint32_t scan = all;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -189,15 +176,10 @@ struct Pass {
       for (int w = 0; w < warps; ++w) sh.counts[w][threadIdx.x] += base;
     }
     __syncthreads();
-    each([&](uint2 e, uint32_t digit, uint32_t same, bool live) {
-      uint32_t at = 0;
-      if (live) at = sh.counts[warp][digit];
-      __syncwarp();
-      if (live) {
-        *reinterpret_cast<uint2*>(dst + at + __popc(same & below)) = e;
-        if ((same & below) == 0u) sh.counts[warp][digit] = at + __popc(same);
-      }
-    });
+    for (int i = threadIdx.x; i < size; i += kSortThreads) {
+      const uint2 e = sh.list[i];
+      *reinterpret_cast<uint2*>(dst + sh.counts[i / part][digit_of(e)] + sh.place[i]) = e;
+    }
   }
 };
 
@@ -534,8 +516,7 @@ cudaError_t launch_embedding_fwd(const Embed& e, cudaStream_t s) {
   return err;
 }
 
-// tokens that the cluster sorts (by it / by launches over all SMs, whole gradient of 64 columns: 65536 63.5 / 66.5 us, 131072 107 / 85, 1000000 483 / 167)
-constexpr int64_t kClusterMost = 65536;
+constexpr int64_t kClusterMost = kSortCtas * kSortTile;  // tokens that the cluster sorts
 int64_t tiles_of(int64_t n) { return n > kClusterMost ? (n + kSortTile - 1) / kSortTile : 0; }
 size_t embedding_bwd_workspace(int64_t n, int64_t cols) {
   return 2 * padded((size_t)n * sizeof(Entry)) + 2 * padded((size_t)chunks_of(n) * cols * 4) + padded((size_t)(tiles_of(n) + 1) * kBins * 4);

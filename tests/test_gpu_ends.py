@@ -163,6 +163,7 @@ def test_heads_of_any_finite_magnitude(magnitude):
 EMBED = [  # tokens, vocabulary, columns, spare columns
     (1, 1, 8, 0), (1, 100, 64, 8), (3, 7, 1000, 0), (33, 5, 136, 8), (257, 50, 2056, 0), (1003, 5003, 264, 16), (4096, 600, 72, 0), (5000, 3, 40, 8),
     (9001, 70001, 16, 0), (40000, 11, 24, 0), (20000, 300000, 8, 8), (70003, 1000, 16, 0), (100000, 600000, 8, 8),
+    (4097, 9000, 8, 0), (32768, 900, 8, 0), (32769, 900, 8, 8),  # where the ways to sort change
 ]
 
 
