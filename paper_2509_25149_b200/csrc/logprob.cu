@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
 constexpr int kRing = 5, kStage = kThreads * 32;  // what is on its way to a CTA: 32 bytes a thread and stage
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kLowest = -3.402823466e38f, kFar = -300.f, kReach = 400.f;
+constexpr float kLn2 = 0.69314718055994530942f, kLowest = -3.402823466e38f, kFar = -300.f, kReach = 400.f;
 
 __device__ __forceinline__ float exp2_fast(float v) {
   float r;
@@ -48,7 +48,7 @@ struct Fwd {
   int* top_ids;
   float* top_logprobs;
   int64_t rows, vocab, ld;
-  float scale;
+  float scale, per;  // per: scale in powers of two, rounded once
   int top;
 };
 
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
   const uint8_t* const x = static_cast<const uint8_t*>(a.logits) + row * a.ld * (F32 ? 4 : 2);
   const int64_t whole = a.vocab / E, chunks = (a.vocab + E - 1) / E;
   const int64_t c0 = chunks * part / parts, c1 = chunks * (part + 1) / parts, full = min(c1, whole);
-  const float per = a.scale * kLog2e, reach = kReach / per;
+  const float per = a.per, reach = kReach / per;
   Running<F32, ENTROPY> run(per);
   // the row comes through a ring in which every thread has places of its own
   const uint32_t mine = smem_u32(smem) + threadIdx.x * 16;
@@ -461,7 +461,7 @@ struct Bwd {
   const float* dentropy;
   void* dlogits;
   int64_t rows, vocab, ld, lddl, dcols, steps, per_row;
-  float scale;
+  float scale, per;
 };
 constexpr int kBwdCtas = 148 * 4, kBwdSteps = 32;  // as many as are resident; steps of a warp where there are more
 
@@ -492,7 +492,7 @@ struct RowGrad {
     const int64_t t = g.targets.p ? g.targets[row] : -1;
     const float w = g.dlogprob ? g.dlogprob[row] * g.scale : 0.f, e = ENTROPY ? g.dentropy[row] * g.scale : 0.f, h = ENTROPY ? g.entropy[row] : 0.f;
     const bool empty = st.x == minus_infinity(), there = t >= 0 && t < g.vocab && !empty;
-    const float m = empty ? 0.f : st.x, per = g.scale * kLog2e;  // (all of an empty row is p = 0 then)
+    const float m = empty ? 0.f : st.x, per = g.per;  // (all of an empty row is p = 0 then)
     at = Reference(m, per);
     least = Chunk<F32>::held(m - kReach / per);
     total = empty ? 0.f : st.y;
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_bwd_kernel(const Bwd a) {
   now.load<F32, ENTROPY>(a, row);
   then = now;
   if (row + 1 < a.rows) then.load<F32, ENTROPY>(a, row + 1);
-  const float per = a.scale * kLog2e;
+  const float per = a.per;
   auto distance = [&](float v) { return __uint_as_float(max_nan(__float_as_uint(now.at.distance(v, per)), __float_as_uint(-kReach))); };
   auto grad = [&](float2 v) {  // of distances
     const float2 l = add2(v, both(-now.total)), p = make_float2(exp2_fast(l.x), exp2_fast(l.y));
@@ -651,6 +651,8 @@ cudaError_t launch_bwd(const Bwd& a, cudaStream_t s) {
   return launch_divided(100, kern, dim3(ctas), dim3(kThreads), kRing * kStage, s, a);
 }
 
+float in_powers_of_two(float scale) { return (float)((double)scale * 1.44269504088896340736); }
+
 }  // namespace
 
 cudaError_t launch_logprob_fwd(const Logprob& l, cudaStream_t s) {
@@ -662,6 +664,7 @@ cudaError_t launch_logprob_fwd(const Logprob& l, cudaStream_t s) {
   a.top_ids = l.top_ids; a.top_logprobs = l.top_logprobs;
   a.rows = l.rows; a.vocab = l.vocab; a.ld = l.ld;
   a.scale = l.scale;
+  a.per = in_powers_of_two(l.scale);
   a.top = l.top;
   const bool top = l.top_ids || l.top_logprobs;
   cudaError_t e;
@@ -687,6 +690,7 @@ cudaError_t launch_logprob_bwd(const Logprob& l, cudaStream_t s) {
   a.per_row = (l.dcols + of_step - 1) / of_step;
   a.steps = l.rows * a.per_row;
   a.scale = l.scale;
+  a.per = in_powers_of_two(l.scale);
   const cudaError_t e = l.fp32 ? (l.out_fp32 ? launch_bwd<true, true>(a, s) : launch_bwd<true, false>(a, s))
                                : (l.out_fp32 ? launch_bwd<false, true>(a, s) : launch_bwd<false, false>(a, s));
   count_launch();
