@@ -51,6 +51,10 @@ HEADS = [  # rows, query heads, key heads, width, rotated, neighbours, positions
     (300, 7, 2, 256, 256, False, "rows", 0),
     (40, 3, 1, 256, 128, True, "before", 8),
     (2500, 8, 2, 128, 64, False, "rows", 256),
+    # every place of a step filled, one and two heads to a lane, all widths of a group
+    (64, 2, 2, 128, 128, True, "far", 0), (64, 2, 2, 128, 0, False, "rows", 8), (64, 4, 0, 64, 64, False, "rows", 0), (50, 1, 1, 256, 256, False, "rows", 0),
+    (50, 2, 2, 256, 64, True, "rows", 0), (50, 8, 8, 64, 64, True, "before", 64), (50, 16, 16, 32, 32, False, "rows", 0), (50, 8, 8, 32, 16, True, "rows", 0),
+    (50, 0, 16, 32, 16, False, "rows", 0), (3000, 8, 0, 128, 0, False, "rows", 0),
 ]
 
 
@@ -285,6 +289,7 @@ def logits_of(rows, vocab, kind, dtype, seed=1):
 
 LOGITS = [(rows, vocab, "plain") for rows, vocab in ((1, 1), (3, 2), (5, 7), (2, 8), (4, 33), (3, 1000), (2, 4097), (700, 257), (9, 32768), (2, 50257), (1, 131072), (160, 9000))]
 LOGITS += [(5, vocab, kind) for kind in ("masked", "few", "lowest", "equal", "steps", "rising", "large", "sure", "columns") for vocab in (100, 5001, 70000)]
+LOGITS += [(2049, 4104, "masked"), (2049, 4099, "steps"), (2048, 4200, "equal")]  # many rows of more than 4096: a warp takes each
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32], ids=str)
