@@ -5,10 +5,11 @@
 // gradient reads it once more and writes: 8192 x 131072 in bf16 350 us (94 % of the copy rate) and 647 (101 %), in a long run 416 and 657.  There the GPU is
 // at its power limit, at 1.5 GHz for 1.96, and what an element costs in instructions tells: everything is in powers of two, z log2(e) = x per, and a
 // difference is one fused multiply-add, d = x per - ref.
-//   ref is the binary32 number nearest to m per, and what the sums are relative to: no rounding of m per is in any difference
-//   (one that all elements have in common would be, times the distance of the logits from zero).
+//   ref is the binary32 number nearest to m per, and what the sums are relative to: its rounding is the same in all differences of a row, which it
+//   moves by half a power of two at most, since this form is for |m per| <= 2^24.  Rows whose largest logit is beyond that, those that are masked with a large
+//   finite number, say, take differences of the logits as they are, (x - m) per.
 //   Logits more than 400 powers of two below the largest are taken for that far: p is 0 there all the same, and minus infinity has a finite
-//   difference, so that p d is 0 too.  Rows whose largest logit is beyond 2^90, those of the type's lowest values, say, take differences of the logits as they are.
+//   difference, so that p d is 0 too.
 #include <algorithm>
 
 #include "around.h"
@@ -105,23 +106,22 @@ struct Chunk {
   }
 };
 
-constexpr float kNear = 0x1p90f;
+constexpr float kNear = 0x1p24f;  // powers of two: what m per rounds off is far below those that 2^d has room for, and m - 400 / per is not m
 
 // What a row's differences are taken from: its largest logit (of the elements so far), m, minus infinity where there is none
 struct Reference {
   float from, ref;  // near: 0 and fl(m per);  far: max(m, lowest) and 0
   bool near;
   __device__ __forceinline__ Reference(float m, float per) {
-    near = fabsf(m) <= kNear;
+    ref = m * per;
+    near = fabsf(ref) <= kNear;
     from = near ? 0.f : fmaxf(m, kLowest);
-    ref = near ? m * per : 0.f;
+    ref = near ? ref : 0.f;
   }
   // of a logit, in powers of two
-  __device__ __forceinline__ float distance(float x, float per) const { return near ? fmaf(x, per, -ref) : (x - from) * per; }
-  // of what another reference stands for
-  __device__ __forceinline__ float distance(const Reference& r, float per) const {
-    return near && r.near ? r.ref - ref : ((r.near ? r.ref / per : r.from) - (near ? ref / per : from)) * per;
-  }
+  __device__ __forceinline__ float distance(float x, float per) const { return fmaf(x - from, per, -ref); }
+  // of what another reference stands for, which is from + ref / per
+  __device__ __forceinline__ float distance(const Reference& r, float per) const { return fmaf(r.from - from, per, r.ref - ref); }
 };
 
 // What a lane holds of its elements: the largest logit m, and the sums of 2^d and d 2^d

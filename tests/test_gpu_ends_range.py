@@ -1,0 +1,91 @@
+"""The operators at the ends of a training step over the whole range of what they accept: logits and scales of any finite size."""
+import math
+
+import pytest
+import torch
+
+import ends_ref as R
+from around_ref import guarded
+from ends_ref import HALF, U, normal
+from paper_2509_25149_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+def new(*shape, dtype=FP32):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda") if dtype.is_floating_point else torch.full(shape, -7, dtype=dtype, device="cuda")
+
+
+# ----------------------------------------------------------------------------------------------- logprob ----
+SIZES = [1e5, 5e6, 1.3e7, 1e8, 1e9, 3e9, 1e10, 1.2e10, 1e12, 1e20, 2.0 ** 90 * (1 - 2.0 ** -7), 2.0 ** 90, 2.0 ** 90 * (1 + 2.0 ** -7)]
+KINDS = ["equal", "equal below", "one", "half below", "around", "around below", "up", "close"]
+
+
+def far_logits(kind, vocab, dtype, seed=1):
+    """A row to each size."""
+    size = torch.tensor(SIZES, dtype=torch.float64)[:, None]
+    x = normal((len(SIZES), vocab), seed, 3.0, torch.float64)
+    if kind == "equal":
+        x = size.expand(-1, vocab)
+    elif kind == "equal below":  # every token is masked with a finite number
+        x = -size.expand(-1, vocab)
+    elif kind == "one":
+        x = torch.zeros_like(x)
+        x[:, vocab // 3] = size[:, 0]
+    elif kind == "half below":
+        x = torch.where(torch.arange(vocab) % 2 == 0, x, -size)
+    elif kind in ("around", "around below"):
+        x = (1 + 0.01 * x) * (size if kind == "around" else -size)
+    elif kind == "up":  # from small to large: the row's maximum grows over the whole range
+        x = torch.exp(torch.linspace(0, 1, vocab, dtype=torch.float64) * size.log())
+    else:  # the largest ones differ by little in binary32, by a step or none in bf16
+        x = size * (1 - torch.arange(vocab, dtype=torch.float64) % 37 * 2.0 ** -22)
+    return x.to(dtype)
+
+
+# rows of a warp, of a CTA (repeated so that there are many), of clusters
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=str)
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1e6, 1e8, 2.0 ** 27, 2.0 ** -60], ids=str)
+@pytest.mark.parametrize("vocab, times", [(100, 1), (4500, 12), (5001, 1), (40003, 1)])
+def test_logits_of_any_finite_size(vocab, times, scale, dtype):
+    wide = (vocab + 7) // 8 * 8 + 8
+    for kind in KINDS:
+        x = far_logits(kind, vocab, dtype)
+        rows, many = len(x), len(x) * times
+        ref = R.Softmax(x, scale)
+        targets = torch.randint(0, vocab, (rows,), generator=torch.Generator().manual_seed(7))
+        targets[0], targets[-1], targets[1] = vocab // 3, vocab - 1, -1
+        there = targets >= 0
+        xs, tg = guarded(many, vocab, dtype, wide, x.repeat(times, 1))[0], targets.repeat(times).cuda()
+        lp, lse, stats, entropy = new(many), new(many), new(many, 2), new(many)
+        B.nvfp4_logprob_fwd(xs, tg, lp, lse, stats, entropy, scale=scale)
+        alone_lp, alone_lse, alone_stats = new(many), new(many), new(many, 2)
+        B.nvfp4_logprob_fwd(xs, tg, alone_lp, alone_lse, alone_stats, scale=scale)
+        top = min(5, vocab)
+        ids, tops = new(many, top, dtype=torch.int32), new(many, top)
+        B.nvfp4_logprob_fwd(xs, top_ids=ids, top_logprobs=tops, scale=scale)
+        # A log probability: roundings of the difference, of the scale in powers of two, of their product, of the sum's logarithm beside it,
+        # of ln 2 and of the product with that, beside what the sum is off by.
+        off = ref.sum_off[:, None] + 6 * U * (ref.surprise + ref.log_total.abs())
+        at = torch.where(there, targets, 0)[:, None]
+        want_lp, lp_off = torch.where(there, ref.log_p.gather(1, at)[:, 0], 0.0), torch.where(there, off.gather(1, at)[:, 0], 0.0)
+        first = R.top_of(x, top)
+        for k in sorted({0, times - 1}):
+            part = slice(k * rows, (k + 1) * rows)
+            for a, b in ((lp, lse), (alone_lp, alone_lse)):
+                R.assert_within(a[part], want_lp, lp_off, f"{kind}: logprob")
+                R.assert_within(b[part], ref.lse, ref.lse_off, f"{kind}: lse")
+            R.assert_within(entropy[part], ref.entropy, ref.entropy_off, f"{kind}: entropy")
+            assert torch.equal(stats[part, 0].cpu(), x.float().max(1).values)
+            assert torch.equal(ids[part].cpu().long(), first), kind
+            R.assert_within(tops[part], ref.log_p.gather(1, first), off.gather(1, first), f"{kind}: top_logprobs")
+        dlp, de = normal((rows,), 8, 1.0, FP32), normal((rows,), 9, 0.3, FP32)
+        for a, b, st in ((dlp, None, alone_stats), (None, de, stats), (dlp, de, stats)):
+            c = lambda t: None if t is None else t.repeat(times).cuda()
+            grad, tol = ref.grad(targets, a, b, scale)
+            for out_dtype in (BF16, FP32):
+                out = guarded(many, vocab, out_dtype, wide)[0]
+                B.nvfp4_logprob_bwd(xs, None if a is None else tg, st, out, c(a), None if b is None else entropy, c(b), scale)
+                for k in sorted({0, times - 1}):
+                    R.assert_within(out[k * rows:(k + 1) * rows], grad, tol + HALF[out_dtype] * (grad.abs() + tol) + 1e-38, f"{kind}: dlogits")
