@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
     const float log_total = log2f(s);
     auto log_p = [&](float v) {
       const float d = ref.distance(v, per);
-      if (s == 0.f) return minus_infinity();
+      if (!(s > 0.f)) return s == 0.f ? minus_infinity() : s;  // (NaN where the row has one, whatever is at v)
       // (far out, nothing beside the difference counts, which may fit binary32 while that many powers of two do not)
       return d < -0x1p60f ? (v - fmaxf(m, kLowest)) * a.scale : kLn2 * (d - log_total);
     };
@@ -491,8 +491,8 @@ struct RowGrad {
     const float2 st = g.stats[row];
     const int64_t t = g.targets.p ? g.targets[row] : -1;
     const float w = g.dlogprob ? g.dlogprob[row] * g.scale : 0.f, e = ENTROPY ? g.dentropy[row] * g.scale : 0.f, h = ENTROPY ? g.entropy[row] : 0.f;
-    const bool empty = st.x == minus_infinity(), there = t >= 0 && t < g.vocab && !empty;
-    const float m = empty ? 0.f : st.x, per = g.per;  // (all of an empty row is p = 0 then)
+    const bool empty = st.x == minus_infinity() && st.y == minus_infinity(), there = t >= 0 && t < g.vocab && !empty;
+    const float m = empty ? 0.f : st.x, per = g.per;  // (all of an empty row is p = 0 then; a NaN beside minus infinities is in the sum)
     at = Reference(m, per);
     least = Chunk<F32>::held(m - kReach / per);
     total = empty ? 0.f : st.y;

@@ -89,3 +89,28 @@ def test_logits_of_any_finite_size(vocab, times, scale, dtype):
                 B.nvfp4_logprob_bwd(xs, None if a is None else tg, st, out, c(a), None if b is None else entropy, c(b), scale)
                 for k in sorted({0, times - 1}):
                     R.assert_within(out[k * rows:(k + 1) * rows], grad, tol + HALF[out_dtype] * (grad.abs() + tol) + 1e-38, f"{kind}: dlogits")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=str)
+@pytest.mark.parametrize("rows, vocab", [(5, 1000), (160, 9000), (5, 9000), (5, 40000)])
+def test_a_nan_among_logits_that_are_ruled_out(rows, vocab, dtype):
+    """Rows 0 to 2 have a NaN: beside nothing but minus infinities; beside a target of minus infinity; beside a target far below.  Rows from 3 on have none."""
+    x = normal((rows, vocab), 1, 2.0, dtype)
+    x[0] = -math.inf
+    x[0, 5] = math.nan
+    x[1:3, vocab // 3] = math.nan
+    x[1, 7], x[2, 7], x[3, 7] = -math.inf, torch.finfo(dtype).min, -math.inf
+    x[4] = -math.inf
+    z, tg, w = x.cuda(), torch.full((rows,), 7, device="cuda"), torch.ones(rows, device="cuda")
+    bad = torch.arange(rows, device="cuda") < 3
+    for with_entropy in (False, True):
+        lp, lse, st, en, dz = new(rows), new(rows), new(rows, 2), new(rows) if with_entropy else None, torch.zeros_like(z)
+        ids, tops = new(rows, 5, dtype=torch.int32), new(rows, 5)
+        B.nvfp4_logprob_fwd(z, tg, lp, lse, st, en, ids, tops)
+        for t in (lp, lse, en, tops[:, 0], tops[:, 4]):
+            assert t is None or torch.equal(torch.isnan(t), bad)
+        assert int(ids.min()) >= 0 and int(ids.max()) < vocab
+        assert bool(torch.isinf(lp[3:5]).all()) and bool((lp[3:5] < 0).all())
+        for dlogprob, dentropy in ((w, None), (None, w), (w, w)) if with_entropy else ((w, None),):
+            B.nvfp4_logprob_bwd(z, None if dlogprob is None else tg, st, dz, dlogprob, None if dentropy is None else en, dentropy)
+            assert bool(torch.isnan(dz[:3]).all()) and bool(torch.isfinite(dz[3:]).all()) and bool((dz[4] == 0).all())
