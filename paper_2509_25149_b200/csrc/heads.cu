@@ -150,9 +150,8 @@ __device__ __forceinline__ float rsqrt_fast(float v) {  // (of normal numbers: e
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-// 1 / sqrt(mean(x^2) + eps) of the N heads that a lane's group holds.  Finite values whose squares, or the sum of them, binary32 does not hold
-// are multiplied by 2^-70 (one of them is above 2^50 then, and eps nothing beside it), and the result is that of what they are now; `shift` says so.  True where the
-// warp had such a head.
+// 1 / sqrt(mean(x^2) + eps) of the N heads that a lane's group holds.  Finite values whose squares, or the sum of them and eps, binary32 does not hold
+// are multiplied by 2^-70, eps by 2^-140, and the result is that of what they are now; `shift` says so.  True where the warp had such a head.
 template <int G, int N>
 __device__ __forceinline__ bool rstd_of(const Args& a, float2 (&x)[N][4], float (&rstd)[N], float (*shift)[N] = nullptr) {
   float sum[N];
@@ -165,8 +164,9 @@ __device__ __forceinline__ bool rstd_of(const Args& a, float2 (&x)[N][4], float 
     for (int k = 0; k < N; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], o);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
+    sum[k] = fmaf(sum[k], a.per_elem, a.eps);
     lost |= !(sum[k] <= 3.402823466e38f);
-    rstd[k] = rsqrt_fast(fmaf(sum[k], a.per_elem, a.eps));
+    rstd[k] = rsqrt_fast(sum[k]);
   }
   if (__builtin_expect(!__any_sync(0xffffffffu, lost), 1)) return false;
 #pragma unroll
@@ -177,7 +177,7 @@ __device__ __forceinline__ bool rstd_of(const Args& a, float2 (&x)[N][4], float 
     for (int j = 0; j < 4; ++j) w[j] = mul2(x[k][j], both(0x1p-70f));
     const float scaled = head_sum<G>(dot8(w, w));
     if (!far) continue;
-    rstd[k] = rsqrt_fast(scaled * a.per_elem);
+    rstd[k] = rsqrt_fast(fmaf(scaled, a.per_elem, a.eps * 0x1p-140f));
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[k][j] = w[j];
     if (shift) (*shift)[k] = 0x1p-70f;

@@ -114,3 +114,38 @@ def test_a_nan_among_logits_that_are_ruled_out(rows, vocab, dtype):
         for dlogprob, dentropy in ((w, None), (None, w), (w, w)) if with_entropy else ((w, None),):
             B.nvfp4_logprob_bwd(z, None if dlogprob is None else tg, st, dz, dlogprob, None if dentropy is None else en, dentropy)
             assert bool(torch.isnan(dz[:3]).all()) and bool(torch.isfinite(dz[3:]).all()) and bool((dz[4] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------------- heads ----
+LARGEST = torch.finfo(FP32).max
+
+
+@pytest.mark.parametrize("dim", [16, 128, 256])
+@pytest.mark.parametrize("eps", [1.0, 1e30, 1e38, 3e38, LARGEST], ids=str)
+def test_heads_with_a_large_eps(eps, dim):
+    """Sums of squares on both sides of the largest binary32 number, beside an eps of their size."""
+    sizes = torch.tensor([1.0, 1e15, 1e17, 5e17, 1e18, 2e18, 5e18, 1e19, 3e19, 1e20, 1e22, 1e30, 3e38], dtype=torch.float64)
+    hq, hk = 2, 1
+    rows, cols = len(sizes), (hq + hk) * dim
+    x = (normal((rows, cols), 5, 0.5, torch.float64).clamp(-1, 1) * sizes[:, None]).to(BF16)
+    eps = float(torch.tensor(eps, dtype=FP32))
+    f, dy = torch.exp(-torch.arange(8) * 0.5).float(), normal((rows, cols), 6)
+    gain = 1 + normal((dim,), 7, 0.2, FP32)
+    leaves = [t.double().requires_grad_() for t in (x, gain, gain)]
+    want = R.heads_fwd(leaves[0], hq, hk, leaves[1], leaves[2], eps, f, torch.arange(rows), False)
+    want.backward(dy.double())
+    u = R.heads_fwd(x.double(), hq, hk, gain, gain, eps, None, None, False).unflatten(1, (hq + hk, dim))
+    y, dx, dgq, dgk = torch.empty_like(x, device="cuda"), torch.empty_like(x, device="cuda"), new(dim), new(dim)
+    ws = torch.empty(B.nvfp4_headnorm_bwd_workspace_bytes(rows, hq, hk, dim), dtype=torch.uint8, device="cuda")
+    B.nvfp4_headnorm_fwd(x.cuda(), hq, hk, y, gain.cuda(), gain.cuda(), eps, f.cuda())
+    B.nvfp4_headnorm_bwd(dy.cuda(), x.cuda(), hq, hk, dx, gain.cuda(), gain.cuda(), eps, dgq, dgk, ws, f.cuda())
+    # the bounds of the ordinary heads: roundings of the sum of squares, the root, sine and cosine, and those of the sums in the gradient
+    R.assert_within(y, want, HALF[BF16] * want.abs() + 2.0 ** -19 * R.beside(u, 16, False).flatten(1) + 2.0 ** -134, "y")
+    h = x.double().unflatten(1, (hq + hk, dim))
+    rstd = 1 / (h.square().mean(2, keepdim=True) + eps).sqrt()
+    n, d = h * rstd, R.beside(dy.double().unflatten(1, (hq + hk, dim)), 16, False)
+    reach = rstd * (d * gain.abs() + n.abs() * (d * gain.abs() * n.abs()).mean(2, keepdim=True))
+    R.assert_within(dx, leaves[0].grad, HALF[BF16] * leaves[0].grad.abs() + 2.0 ** -18 * reach.flatten(1) + 2.0 ** -134, "dx")
+    of = (d * n.abs()).sum(0)
+    R.assert_within(dgq, leaves[1].grad, 2.0 ** -16 * of[:hq].sum(0), "dgain_q")
+    R.assert_within(dgk, leaves[2].grad, 2.0 ** -16 * of[hq:].sum(0), "dgain_k")
