@@ -271,10 +271,11 @@ __global__ void __launch_bounds__(kThreads, 2) headnorm_fwd_kernel(const Args a)
     for (int k = 0; k < N; ++k) {
       float2 out[4];
 #pragma unroll
+      for (int j = 0; j < 4; ++j) v[k][j] = mul2(v[k][j], both(rstd[k]));  // (first: x gain may be too small for binary32)
+#pragma unroll
       for (int j = 0; j < 4; ++j) {
         out[j] = mul2(v[k][j], gc[j]);
         if (MODE != kPlain) out[j] = fma2(l.partner(v[k], j), gs[j], out[j]);
-        out[j] = mul2(out[j], both(rstd[k]));
       }
       if (FULL || (l.live && at.h + k * kHeads < at.heads(a))) l.store(to + k * head, out);
     }

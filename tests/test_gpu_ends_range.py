@@ -149,3 +149,18 @@ def test_heads_with_a_large_eps(eps, dim):
     of = (d * n.abs()).sum(0)
     R.assert_within(dgq, leaves[1].grad, 2.0 ** -16 * of[:hq].sum(0), "dgain_q")
     R.assert_within(dgk, leaves[2].grad, 2.0 ** -16 * of[hq:].sum(0), "dgain_k")
+
+
+@pytest.mark.parametrize("rotary", [0, 32])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_small_heads_with_small_gains(interleaved, rotary):
+    """x gain is below the smallest normal binary32 number, x gain / rms is not."""
+    rows, hq, hk, dim, eps = 7, 2, 1, 32, 2.0 ** -126
+    x = (normal((rows, (hq + hk) * dim), 5, 1.0, torch.float64) * 2.0 ** -119).to(BF16)
+    gain = ((1 + normal((dim,), 7, 0.2, torch.float64)) * 2.0 ** -26).float()
+    f = torch.exp(-torch.arange(rotary // 2) * 0.5).float() if rotary else None
+    want = R.heads_fwd(x.double(), hq, hk, gain, gain, eps, f, torch.arange(rows), interleaved)
+    u = R.heads_fwd(x.double(), hq, hk, gain, gain, eps, None, None, False).unflatten(1, (hq + hk, dim))
+    y = torch.empty_like(x, device="cuda")
+    B.nvfp4_headnorm_fwd(x.cuda(), hq, hk, y, gain.cuda(), gain.cuda(), eps, None if f is None else f.cuda(), interleaved=interleaved)
+    R.assert_within(y, want, HALF[BF16] * want.abs() + 2.0 ** -19 * R.beside(u, rotary, interleaved).flatten(1), "y")
