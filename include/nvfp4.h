@@ -447,7 +447,7 @@ NVFP4_API nvfp4_status nvfp4_embedding_bwd(const void* tokens, int32_t tokens_ar
  *   the columns from vocab to dcols (>= vocab: what the product behind it reads) set to zero.
  *   stats, entropy as the forward call wrote them (entropy only with dentropy).  dlogprob (with targets), dentropy: binary32 [rows], either may be NULL,
  *   not both.  Padded targets take no part in dlogprob.  Rows of nothing but minus infinities get zeros.
- *   dlogits may be the logits themselves (same type and leading dimension).
+ *   dlogits may be the logits themselves (same type and, from two rows on, leading dimension).
  */
 #define NVFP4_TOP_MAX 32
 NVFP4_API nvfp4_status nvfp4_logprob_fwd(const void* logits, int32_t logits_are_fp32, int64_t ld, int64_t rows, int64_t vocab,

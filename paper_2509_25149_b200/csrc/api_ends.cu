@@ -203,7 +203,7 @@ nvfp4_status nvfp4_logprob_bwd(const void* logits, int32_t logits_are_fp32, int6
   if (dcols < vocab || dcols > kMost + 8) return NVFP4_ERR_SHAPE;
   if ((st = check_matrix(dlogits, lddl, dcols, l.out_fp32)) != NVFP4_OK) return st;
   if (!aligned(dlogprob, 4) || !aligned(dentropy, 4)) return NVFP4_ERR_ALIGN;
-  if (dlogits == logits && (l.fp32 != l.out_fp32 || ld != lddl)) return NVFP4_ERR_ARG;
+  if (dlogits == logits && (l.fp32 != l.out_fp32 || (rows > 1 && ld != lddl))) return NVFP4_ERR_ARG;  // (a single row has no next one)
   return status_of(launch_logprob_bwd(l, static_cast<cudaStream_t>(cuda_stream)));
 }
 

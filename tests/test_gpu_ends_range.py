@@ -164,3 +164,18 @@ def test_small_heads_with_small_gains(interleaved, rotary):
     y = torch.empty_like(x, device="cuda")
     B.nvfp4_headnorm_fwd(x.cuda(), hq, hk, y, gain.cuda(), gain.cuda(), eps, None if f is None else f.cuda(), interleaved=interleaved)
     R.assert_within(y, want, HALF[BF16] * want.abs() + 2.0 ** -19 * R.beside(u, rotary, interleaved).flatten(1), "y")
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=str)
+@pytest.mark.parametrize("rows", [1, 2])
+def test_gradient_over_the_logits_with_more_columns(rows, dtype):
+    """The logits are the first columns of what the product wrote, and their gradient goes over all of them, one row too."""
+    vocab, wide = 1003, 1024
+    x = normal((rows, wide), 3, 2.0, dtype).cuda()
+    tg, w, st = torch.arange(rows, device="cuda"), torch.ones(rows, device="cuda"), new(rows, 2)
+    B.nvfp4_logprob_fwd(x[:, :vocab], tg, stats=st)
+    want = new(rows, wide, dtype=dtype)
+    B.nvfp4_logprob_bwd(x[:, :vocab], tg, st, want, w)
+    assert bool((want[:, vocab:] == 0).all()) and bool(torch.isfinite(want).all())
+    B.nvfp4_logprob_bwd(x[:, :vocab], tg, st, x, w)
+    assert torch.equal(x, want)
