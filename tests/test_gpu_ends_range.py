@@ -1,4 +1,5 @@
-"""The operators at the ends of a training step over the whole range of what they accept: logits and scales of any finite size."""
+"""The operators at the ends of a training step over the whole range of what they accept, logits and scales of any finite size among it, and behind the
+library's own kernels."""
 import math
 
 import pytest
@@ -179,3 +180,75 @@ def test_gradient_over_the_logits_with_more_columns(rows, dtype):
     assert bool((want[:, vocab:] == 0).all()) and bool(torch.isfinite(want).all())
     B.nvfp4_logprob_bwd(x[:, :vocab], tg, st, x, w)
     assert torch.equal(x, want)
+
+
+# ------------------------------------------------------------------------------------------------- order ----
+@pytest.mark.parametrize("n", [1, 5000, 40000])  # one launch for the order, a cluster, many launches
+@pytest.mark.parametrize("reader", ["embedding", "norm"])
+def test_a_table_is_read_to_its_end_before_it_is_zeroed(reader, n):
+    """The reader is one of the library's own kernels, which lets the next launch begin early; the call behind it writes zeros beside its sort."""
+    vocab, cols = 40000, 2048
+    tokens, dout = torch.arange(n, device="cuda") % vocab, torch.ones((n, cols), dtype=BF16, device="cuda")
+    ws = torch.empty(B.nvfp4_embedding_bwd_workspace_bytes(n, vocab, cols), dtype=torch.uint8, device="cuda")
+    table, all_rows = torch.empty((vocab, cols), device="cuda"), torch.arange(vocab, device="cuda").flip(0)
+    out, total = torch.empty((vocab, cols), device="cuda"), new(1, dtype=torch.float64)
+    held, ws_n = B.grad_list([table]), torch.empty(B.nvfp4_grad_sq_norm_workspace_bytes(), dtype=torch.uint8, device="cuda")
+
+    def both():
+        if reader == "embedding":
+            B.nvfp4_embedding_fwd(all_rows, table, out)
+        else:
+            B.nvfp4_grad_sq_norm(held, total, ws_n)
+        B.nvfp4_embedding_bwd(tokens, dout, table, ws)
+
+    def check():
+        assert bool((out == 2.0).all()) if reader == "embedding" else float(total) == 4.0 * vocab * cols
+        assert float(table.sum(dtype=torch.float64)) == float(n * cols)
+
+    table.fill_(2.0)
+    both()
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(5):
+        table.fill_(2.0)
+        out.zero_()
+        total.zero_()
+        graph.replay()
+        check()
+        table.fill_(2.0)
+        both()
+        check()
+
+
+def test_log_probabilities_on_two_streams():
+    """Outputs of their own for each call, forward and backward in turn, beside another stream's."""
+    def call(seed):
+        z, tg, w = normal((9, 70000), seed, 3.0).cuda(), torch.arange(9, device="cuda") * 1000, normal((9,), seed + 1, 1.0, FP32).cuda()
+        outs = [new(9), new(9), new(9, 2), new(9), new(9, 12, dtype=torch.int32), new(9, 12), torch.empty_like(z)]
+
+        def run():
+            B.nvfp4_logprob_fwd(z, tg, *outs[:6])
+            B.nvfp4_logprob_bwd(z, tg, outs[2], outs[6], w, outs[3], w)
+
+        return run, outs
+
+    sets, want = [call(1), call(50)], []
+    for run, outs in sets:
+        run()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in outs])
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(10):
+        for _, outs in sets:
+            for t in outs:
+                t.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for (run, _), stream in zip(sets, streams):
+                with torch.cuda.stream(stream):
+                    run()
+        torch.cuda.synchronize()
+        for (_, outs), right in zip(sets, want):
+            assert all(torch.equal(a, b) for a, b in zip(outs, right))
