@@ -412,8 +412,8 @@ __global__ void __launch_bounds__(kThreads, 4) logprob_fwd_kernel(const Fwd a) {
     auto log_p = [&](float v) {
       const float d = ref.distance(v, per);
       if (!(s > 0.f)) return s == 0.f ? minus_infinity() : s;  // (NaN where the row has one, whatever is at v)
-      // (far out, nothing beside the difference counts, which may fit binary32 while that many powers of two do not)
-      return d < -0x1p60f ? (v - fmaxf(m, kLowest)) * a.scale : kLn2 * (d - log_total);
+      // (far out, nothing beside the difference counts; its product with the scale may fit binary32 where that many powers of two, or the difference, do not)
+      return d < -0x1p60f ? (0.5f * v - 0.5f * fmaxf(m, kLowest)) * a.scale * 2.f : kLn2 * (d - log_total);
     };
     if (tid == 0) {
       if (a.lse) a.lse[row] = fmaf(fmaxf(m, kLowest), a.scale, kLn2 * log_total);

@@ -252,3 +252,24 @@ def test_log_probabilities_on_two_streams():
         torch.cuda.synchronize()
         for (_, outs), right in zip(sets, want):
             assert all(torch.equal(a, b) for a, b in zip(outs, right))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=str)
+@pytest.mark.parametrize("scale", [0.25, 2.0 ** -30, 2.0 ** -60], ids=str)
+@pytest.mark.parametrize("vocab", [9, 5001, 70000])
+def test_logits_further_apart_than_the_largest_number(vocab, scale, dtype):
+    """The difference of two logits is beyond binary32, its product with the scale is not."""
+    x = torch.zeros((3, vocab), dtype=torch.float64)
+    x[:, 0] = 3e38
+    x[0, 1], x[1, vocab - 1], x[2, 1:] = -3e38, -2.5e38, -3.3e38
+    x, targets = x.to(dtype), torch.tensor([1, vocab - 1, 4])
+    xs = guarded(3, vocab, dtype, (vocab + 7) // 8 * 8, x)[0]
+    lp, lse, entropy, ids, tops = new(3), new(3), new(3), new(3, 9, dtype=torch.int32), new(3, 9)
+    B.nvfp4_logprob_fwd(xs, targets.cuda(), lp, lse, None, entropy, ids, tops, scale=scale)
+    z = x.double() * scale
+    want = z - z[:, :1]  # (the others' probabilities are 0 even at the smallest scale)
+    assert torch.equal(ids.cpu().long(), R.top_of(x, 9))
+    R.assert_within(lp, want.gather(1, targets[:, None])[:, 0], 4 * U * want.gather(1, targets[:, None])[:, 0].abs(), "logprob")
+    R.assert_within(tops, want.gather(1, R.top_of(x, 9)), 4 * U * want.gather(1, R.top_of(x, 9)).abs(), "top_logprobs")
+    R.assert_within(lse, z[:, 0], 4 * U * z[:, 0].abs(), "lse")
+    assert bool((entropy == 0).all())
