@@ -383,7 +383,7 @@ NVFP4_API nvfp4_status nvfp4_dequantize_bf16(const nvfp4_tensor* t, void* out_bf
  * output head, norms), and what stands between the weight gradients and their use.  Conventions as for the operators around the layers:
  * bf16 leading dimensions are multiples of 8, binary32 ones of 4, pointers 16-byte aligned, cols a multiple of 8, any number of rows from
  * one on, workspaces 256-byte aligned and not shared by calls that may run at the same time, every sum in an order that depends on the
- * sizes and the GPU alone.  Tokens, targets and positions are int32, or int64 where ..._is_int64 is set.
+ * sizes and the GPU alone (that of the embedding's gradient on the tokens too: the same for equal inputs).  Tokens, targets and positions are int32, or int64 where ..._is_int64 is set.
  *
  * nvfp4_headnorm_fwd: the query and key heads of a QKV product.  Row r of x [rows x (heads_q + heads_k) * head_dim] holds the query heads,
  *   then the key heads (what stands behind them in the row, the values, is neither read nor written: ldx says where the next row begins).
@@ -441,12 +441,13 @@ NVFP4_API nvfp4_status nvfp4_embedding_bwd(const void* tokens, int32_t tokens_ar
  *   top_ids (int32), top_logprobs (binary32): [rows x top], the `top` likeliest tokens, likeliest first, equal ones by index; 1 <= top <=
  *   NVFP4_TOP_MAX and <= vocab where either is wanted.
  *   A row of nothing but minus infinities has lse and log probabilities of minus infinity and entropy 0; one with a NaN has NaN in all but the
- *   likeliest tokens' numbers, which are some of [0, vocab), and in its gradient.
+ *   likeliest tokens' numbers, which are some of [0, vocab), and in its gradient.  Logits may be of any finite size at any scale: what z or log p has beyond
+ *   binary32 is infinite.
  * nvfp4_logprob_bwd: the gradient of sum over rows of dlogprob * logprob + dentropy * entropy by the logits:
  *   dlogits = scale * (dlogprob * ((j == target) - p) - dentropy * p * (log p + entropy)), in the type of the logits or the other one (dlogits_is_fp32),
  *   the columns from vocab to dcols (>= vocab: what the product behind it reads) set to zero.
  *   stats, entropy as the forward call wrote them (entropy only with dentropy).  dlogprob (with targets), dentropy: binary32 [rows], either may be NULL,
- *   not both.  Padded targets take no part in dlogprob.  Rows of nothing but minus infinities get zeros.
+ *   not both.  Padded targets take no part in dlogprob.  Rows of nothing but minus infinities get zeros.  Probabilities below 2^-126 count as 0.
  *   dlogits may be the logits themselves (same type and, from two rows on, leading dimension).
  */
 #define NVFP4_TOP_MAX 32

@@ -2,7 +2,7 @@
 //   z = scale logit;  lse = ln sum e^z;  log p = z - lse;  H = - sum p log p
 //   gradient by a logit  scale (dlogprob ((j == target) - p) - dentropy p (log p + H))
 // Bound by HBM: the forward pass reads a row once, with the running maximum and the sums of e^(z - m) and (z - m) e^(z - m) in registers; the
-// gradient reads it once more and writes: 8192 x 131072 in bf16 350 us (94 % of the copy rate) and 647 (101 %), in a long run 416 and 657.  There the GPU is
+// gradient reads it once more and writes: 8192 x 131072 in bf16 339 us (97 % of the copy rate) and 648 (101 %), in a long run 405 and 651.  There the GPU is
 // at its power limit, at 1.5 GHz for 1.96, and what an element costs in instructions tells: everything is in powers of two, z log2(e) = x per, and a
 // difference is one fused multiply-add, d = x per - ref.
 //   ref is the binary32 number nearest to m per, and what the sums are relative to: its rounding is the same in all differences of a row, which it
@@ -616,7 +616,7 @@ unsigned cluster_of(int64_t rows, int64_t vocab) {
 }
 
 // Whether a warp takes a row by itself: it has no barriers to wait at, and takes longer by the row's length.  By one warp / by a CTA, us: 512 x 4096 4.2 / 4.2, 512 x 8192
-// 5.9 / 5.1; 2048 x 8192 9.7 / 14.6, 2048 x 32768 26.3 / 28.4, 16384 x 1000 13.4 / 74, 16384 x 32768 166 / 193; with the likeliest tokens 2048 x 8192 21 / 30,
+// 5.9 / 5.1; 2048 x 8192 9.7 / 14.6, 2048 x 32768 26.3 / 28.4, 16384 x 1000 13.4 / 74, 16384 x 32768 166 / 193; with the eight likeliest tokens 2048 x 8192 21 / 30,
 // 2048 x 16384 38 / 35, 16384 x 16384 151 / 256, 16384 x 32768 345 / 310.
 bool warp_rows(int64_t rows, int64_t vocab, bool top) { return vocab <= 4096 || (rows >= 2048 && vocab <= (top ? 16384 : 32768)); }
 
